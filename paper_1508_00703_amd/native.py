@@ -29,8 +29,11 @@ PDB_SCHED_WALK = 5
 PDB_SCHED_SHORT = 6
 PDB_EPOCH_AUTO, PDB_EPOCH_LEVELS, PDB_EPOCH_SYNCFREE = 0, 1, 2
 PDB_STALE_AUTO, PDB_STALE_SYNCFREE, PDB_STALE_WINDOWED = 0, 1, 2
+PDB_F32, PDB_F16, PDB_BF16 = 0, 1, 2
+PDB_I32, PDB_I64 = 0, 1
+PDB_MAX_TOP, PDB_MAX_TEACHER = 128, 1024
 
-# every symbol declared in include/pdb.h
+# every symbol declared in include/*.h
 EXPORTS = (
     "pdb_strerror", "pdb_last_hip_error", "pdb_schedule_workspace_bytes",
     "pdb_epoch_workspace_bytes", "pdb_schedule", "pdb_sgd_epoch", "pdb_mf_epoch",
@@ -41,6 +44,10 @@ EXPORTS = (
     "pdb_sgd_epoch_noalloc",
     # include/pdb_mb.h
     "pdb_mb_workspace_bytes", "pdb_mb_copy", "pdb_mb_hop", "pdb_mb_barrier",
+    # include/pdb_tokens.h
+    "pdb_embed_lookup", "pdb_embed_grad_workspace_bytes", "pdb_embed_grad",
+    "pdb_token_logprobs_workspace_bytes", "pdb_token_logprobs", "pdb_token_logprobs_grad",
+    "pdb_distill_workspace_bytes", "pdb_distill",
 )
 
 
@@ -141,6 +148,18 @@ def load() -> ctypes.CDLL:
     lib.pdb_mb_hop.argtypes = [i64, i32, P, sz, ctypes.POINTER(ctypes.c_double),
                                ctypes.POINTER(i32), ctypes.POINTER(i32), O, P]
     lib.pdb_mb_barrier.argtypes = [i64, i32, P, sz, ctypes.POINTER(ctypes.c_double), O, P]
+    lib.pdb_embed_lookup.argtypes = [P, i32, i64, i64, i64, P, i32, i64, f32, P, i32, i64, P, P]
+    lib.pdb_embed_grad_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+    lib.pdb_embed_grad.argtypes = [P, i32, i64, P, i32, i64, P, i32, i64, i64, i64, f32, i32, P, P,
+                                   sz, P]
+    lib.pdb_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32, ctypes.POINTER(sz)]
+    lib.pdb_token_logprobs.argtypes = [P, i32, i64, i64, i64, P, i32, f32, P, P, P, i32, P, P, P, P,
+                                       sz, P]
+    lib.pdb_token_logprobs_grad.argtypes = [P, i32, i64, i64, i64, P, i32, f32, P, P, P, P, P, i64,
+                                            P, P]
+    lib.pdb_distill_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.pdb_distill.argtypes = [P, i32, i64, i64, i64, P, P, i32, i32, f32, P, P, P, i64, P, P, sz,
+                                P]
     for name in EXPORTS:
         if name not in ("pdb_strerror",):
             getattr(lib, name).restype = ctypes.c_int
@@ -549,3 +568,248 @@ def pdb_mb_barrier(rounds: int, blocks: int, device, ws=None, stream=None, opt=N
     _check(load().pdb_mb_barrier(rounds, blocks, _ptr(ws), ws.numel(), ctypes.byref(ns),
                                  _opt(opt), _stream(stream, device)), "pdb_mb_barrier")
     return ns.value
+
+
+# ---------------------------------------------------------------------------
+# token operators (include/pdb_tokens.h)
+#
+# Matrices are 2-D tensors with unit column stride and any row stride; tokens
+# are int32 or int64.  status: an int32 device tensor that the caller has
+# cleared, set to PDB_ERR_INVALID_ARG when a token or id is out of range.
+
+_DTYPES = {torch.float32: PDB_F32, torch.float16: PDB_F16, torch.bfloat16: PDB_BF16}
+_INDEXES = {torch.int32: PDB_I32, torch.int64: PDB_I64}
+
+
+def _matrix(t, name):
+    """(address, pdb_dtype, row stride) of a device matrix."""
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError("%s must be float32, float16 or bfloat16" % name)
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % name)
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    rows, cols = t.shape
+    if cols > 1 and rows > 0 and t.stride(1) != 1:
+        raise ValueError("%s must have unit column stride" % name)
+    return t.data_ptr() or None, dt, t.stride(0) if rows > 1 else cols
+
+
+def _vector(t, name, n, dtype=torch.float32):
+    """Address of a contiguous device vector of n elements; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, str(dtype).replace("torch.", "")))
+    if t.numel() != n:
+        raise ValueError("%s must hold %d elements" % (name, n))
+    return _ptr(t)
+
+
+def _tokens(t, n):
+    """(address, pdb_index) of n tokens; (None, PDB_I32) of None."""
+    if t is None:
+        return None, PDB_I32
+    ix = _INDEXES.get(t.dtype)
+    if ix is None:
+        raise TypeError("tokens must be int32 or int64")
+    if t.numel() != n:
+        raise ValueError("tokens must hold %d elements" % n)
+    return _ptr(t), ix
+
+
+def _status(status):
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise TypeError("status must be an int32 device tensor")
+    return _ptr(status)
+
+
+class _Call:
+    """The device and stream of a call, and the tensors allocated for it: those
+    are kept from reuse until the stream is done with them, also where it is not
+    the current one."""
+
+    def __init__(self, device, stream, *tensors):
+        for t in tensors:
+            if t is not None and t.device != device:
+                raise ValueError("tensors on different devices")
+        self.device = device
+        self.other = stream
+        self.guard = None
+        if device.index is not None and device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        self.stream = _stream(self.other, self.device)
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def empty(self, shape, dtype):
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.other is not None:
+            t.record_stream(self.other)
+        return t
+
+    def workspace(self, ws, nbytes):
+        return self.empty(max(nbytes, 1), torch.uint8) if ws is None else ws
+
+
+def pdb_embed_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out=None,
+                     out_dtype=None, status=None, stream=None) -> torch.Tensor:
+    """scale * table[tokens] as a tensor of tokens.shape + (d,); zeros where a
+    token is negative.  out: None, or a matrix of tokens.numel() rows to fill."""
+    tp, tdt, ld = _matrix(table, "table")
+    v, d = table.shape
+    n = tokens.numel()
+    kp, ix = _tokens(tokens, n)
+    with _Call(table.device, stream, tokens, out, status) as c:
+        shaped = out
+        if out is None:
+            shaped = c.empty(tuple(tokens.shape) + (d,), out_dtype or table.dtype)
+            out = shaped.view(n, d)
+        elif tuple(out.shape) != (n, d) or (out_dtype or out.dtype) != out.dtype:
+            raise ValueError("out must be %d x %d (of out_dtype, if given)" % (n, d))
+        op, odt, ldo = _matrix(out, "out")
+        _check(load().pdb_embed_lookup(tp, tdt, ld, v, d, kp, ix, n, scale, op, odt, ldo,
+                                       _status(status), c.stream), "pdb_embed_lookup")
+    return shaped
+
+
+def pdb_embed_grad_workspace_bytes(n: int, v: int, d: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().pdb_embed_grad_workspace_bytes(n, v, d, ctypes.byref(out)),
+           "pdb_embed_grad_workspace_bytes")
+    return out.value
+
+
+def pdb_embed_grad(dy: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,
+                   accumulate: bool = False, ws=None, status=None, stream=None) -> torch.Tensor:
+    """grad[t] = scale * the sum of dy's rows of token t, zeros elsewhere; with
+    accumulate the sums are added to grad (the table itself and scale = -lr: the
+    SGD step on the rows in use).  dy: tokens.shape + (d,), or its matrix."""
+    n = tokens.numel()
+    gp, gdt, ldg = _matrix(grad, "grad")
+    v, d = grad.shape
+    if dy.dim() != 2:
+        dy = dy.view(n, d)
+    yp, ydt, ldy = _matrix(dy, "dy")
+    if tuple(dy.shape) != (n, d):
+        raise ValueError("dy must be %d x %d" % (n, d))
+    kp, ix = _tokens(tokens, n)
+    with _Call(grad.device, stream, dy, tokens, ws, status) as c:
+        ws = c.workspace(ws, pdb_embed_grad_workspace_bytes(n, v, d))
+        _check(load().pdb_embed_grad(yp, ydt, ldy, kp, ix, n, gp, gdt, ldg, v, d, scale,
+                                     1 if accumulate else 0, _status(status), _ptr(ws), ws.numel(),
+                                     c.stream), "pdb_embed_grad")
+    return grad
+
+
+class TokenLogprobs:
+    """Output of pdb_token_logprobs: logp [n], entropy [n], stats [n, 2] (the
+    largest logit and the log of the sum, for the gradient), top_id and
+    top_logp [n, top]; logp is None without tokens, top_* without alternatives."""
+
+    __slots__ = ("logp", "entropy", "stats", "top_id", "top_logp")
+
+    def __init__(self, logp, entropy, stats, top_id, top_logp):
+        self.logp, self.entropy, self.stats = logp, entropy, stats
+        self.top_id, self.top_logp = top_id, top_logp
+
+
+def pdb_token_logprobs_workspace_bytes(n: int, v: int, top: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().pdb_token_logprobs_workspace_bytes(n, v, top, ctypes.byref(out)),
+           "pdb_token_logprobs_workspace_bytes")
+    return out.value
+
+
+def pdb_token_logprobs(logits: torch.Tensor, tokens=None, top: int = 0, temp: float = 1.0, ws=None,
+                       status=None, stream=None) -> TokenLogprobs:
+    """Log probabilities of the given tokens (None: of none) under
+    softmax(logits / temp), the rows' entropies, and the `top` best entries of
+    each row with their log probabilities, ties to the lowest index.  A row
+    whose token is negative is skipped."""
+    zp, zdt, ldz = _matrix(logits, "logits")
+    n, v = logits.shape
+    kp, ix = _tokens(tokens, n)
+    with _Call(logits.device, stream, tokens, ws, status) as c:
+        ws = c.workspace(ws, pdb_token_logprobs_workspace_bytes(n, v, top))
+        f = torch.float32
+        r = TokenLogprobs(None if tokens is None else c.empty(n, f), c.empty(n, f),
+                          c.empty((n, 2), f), c.empty((n, top), torch.int32) if top else None,
+                          c.empty((n, top), f) if top else None)
+        _check(load().pdb_token_logprobs(zp, zdt, ldz, n, v, kp, ix, temp, _ptr(r.logp),
+                                         _ptr(r.entropy), _ptr(r.stats), top, _ptr(r.top_id),
+                                         _ptr(r.top_logp), _status(status), _ptr(ws), ws.numel(),
+                                         c.stream), "pdb_token_logprobs")
+    return r
+
+
+def pdb_token_logprobs_grad(logits: torch.Tensor, tokens, stats: torch.Tensor, d_logp=None,
+                            entropy=None, d_entropy=None, temp: float = 1.0, out=None, status=None,
+                            stream=None) -> torch.Tensor:
+    """The gradient of sum(d_logp * logp) + sum(d_entropy * entropy) by the
+    logits; stats and entropy from pdb_token_logprobs.  out: None, or where it
+    goes (the logits themselves may be given)."""
+    zp, zdt, ldz = _matrix(logits, "logits")
+    n, v = logits.shape
+    kp, ix = _tokens(tokens, n)
+    with _Call(logits.device, stream, tokens, stats, d_logp, entropy, d_entropy, out, status) as c:
+        if out is None:
+            out = c.empty((n, v), logits.dtype)
+        elif out.shape != logits.shape or out.dtype != logits.dtype:
+            raise ValueError("out must have the logits' shape and type")
+        op, _, ldd = _matrix(out, "out")
+        _check(load().pdb_token_logprobs_grad(
+            zp, zdt, ldz, n, v, kp, ix, temp, _vector(stats, "stats", 2 * n),
+            _vector(entropy, "entropy", n), _vector(d_logp, "d_logp", n),
+            _vector(d_entropy, "d_entropy", n), op, ldd, _status(status), c.stream),
+            "pdb_token_logprobs_grad")
+    return out
+
+
+def pdb_distill_workspace_bytes(n: int, v: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().pdb_distill_workspace_bytes(n, v, ctypes.byref(out)),
+           "pdb_distill_workspace_bytes")
+    return out.value
+
+
+def pdb_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temp: float = 1.0,
+                weight=None, grad: bool = True, out=None, ws=None, status=None, stream=None):
+    """(loss [n], dlogits): each row's weighted divergence from the teacher's
+    distribution over its k entries ids [n, k] (int32, negative: no entry) with
+    logits teacher [n, k], and the gradient of the losses' sum by the logits
+    (None without grad).  out: where the gradient goes (the logits themselves
+    may be given)."""
+    zp, zdt, ldz = _matrix(logits, "logits")
+    n, v = logits.shape
+    if ids.dim() != 2 or ids.shape != teacher.shape or ids.shape[0] != n:
+        raise ValueError("ids and teacher must be matrices of %d rows and equal shape" % n)
+    k = ids.shape[1]
+    tdt = _DTYPES.get(teacher.dtype)
+    if tdt is None:
+        raise TypeError("teacher must be float32, float16 or bfloat16")
+    with _Call(logits.device, stream, ids, teacher, weight, out, ws, status) as c:
+        ws = c.workspace(ws, pdb_distill_workspace_bytes(n, v))
+        loss = c.empty(n, torch.float32)
+        op, ldd = None, 0
+        if grad:
+            if out is None:
+                out = c.empty((n, v), logits.dtype)
+            elif out.shape != logits.shape or out.dtype != logits.dtype:
+                raise ValueError("out must have the logits' shape and type")
+            op, _, ldd = _matrix(out, "out")
+        elif out is not None:
+            raise ValueError("out is for the gradient")
+        _check(load().pdb_distill(zp, zdt, ldz, n, v, _vector(ids, "ids", n * k, torch.int32),
+                                  _ptr(teacher), tdt, k, temp, _vector(weight, "weight", n),
+                                  _ptr(loss), op, ldd, _status(status), _ptr(ws), ws.numel(),
+                                  c.stream), "pdb_distill")
+    return loss, out
