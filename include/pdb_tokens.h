@@ -63,8 +63,8 @@ int pdb_embed_grad_workspace_bytes(int64_t n, int64_t v, int64_t d, size_t *byte
  * table itself and scale = -lr times the lookup's scale that is the gradient
  * step of Sec. 2 on the rows that the batch used (Definition 3: every read of
  * the batch before its writes).  grad: device, v x d, row stride ldg, of
- * grad_dtype.  A token's rows are summed in ascending i: in runs that the
- * sizes fix, then the runs in order.  ws: at least
+ * grad_dtype.  A token's rows are summed in ascending i, in runs that the sizes
+ * fix, then the runs' sums.  ws: at least
  * pdb_embed_grad_workspace_bytes(n, v, d). */
 int pdb_embed_grad(const void *dy, int dtype, int64_t ldy, const void *tokens, int index,
                    int64_t n, void *grad, int grad_dtype, int64_t ldg, int64_t v, int64_t d,

@@ -87,27 +87,309 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 }
 
 // ----------------------------------------------------------------------------
-// gradient
+// gradient: tokens in order
+//
+// (token, position) in order, stable.  Few tokens are placed by counting, in one
+// launch.  More go through a radix sort: a block of 1024 threads takes a tile of up
+// to 16 x 1024 tokens, each wave a stretch of it, and ranks them by ballots (a hot
+// token costs nothing extra).  A pass is two launches, the tiles' digit counts and
+// the move, each block summing the counts of all tiles by itself, which takes no
+// scan launches; past kSortTiles that reading grows too long and the library's own
+// sort runs.
 
-// tokens to sort keys: padding goes behind every row of the table
-__global__ __launch_bounds__(kBlock) void k_embed_keys(const void *__restrict__ tokens, int index,
+constexpr int kSortBlock = 1024;
+constexpr int kSortItems = 16;
+constexpr int kSortTile = kSortBlock * kSortItems;
+constexpr int kSortTiles = 512;
+
+struct SortLds {
+    uint32_t key[kSortTile], val[kSortTile];
+    uint32_t cnt[kSortBlock / kWave][256];  // per wave and digit: a count, then where its run starts
+    uint32_t start[256];                    // per digit: where it starts in the tile
+    uint32_t out[256], all[256];            // per digit: where it goes; all tiles' count
+    uint32_t wave[4];
+};
+
+__device__ __forceinline__ uint32_t digit_of(uint32_t key, int shift, int nb) {
+    return (key >> shift) & ((1u << nb) - 1u);
+}
+// The lanes that hold the same digit: of each bit's ballot, or its complement,
+// by the lane's own bit spread over a word.  All 8 bits of a digit are looked at
+// (those above nb are 0): unrolled, they take half the instructions of a loop.
+__device__ __forceinline__ unsigned long long digit_peers(uint32_t dg, bool valid) {
+    const unsigned long long there = __ballot(valid);
+    uint32_t lo = (uint32_t)there, hi = (uint32_t)(there >> 32);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const uint32_t own = (uint32_t)__builtin_amdgcn_sbfe((int)dg, b, 1);
+        const unsigned long long set = __ballot(own != 0);
+        lo &= ~((uint32_t)set ^ own);
+        hi &= ~((uint32_t)(set >> 32) ^ own);
+    }
+    return (unsigned long long)hi << 32 | lo;
+}
+
+// exclusive prefix sum over the first 256 threads of the block
+__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t *s_wave) {
+    const uint32_t incl = wave_incl_scan_u32(v);
+    const int w = wave_in_block();
+    if (w < 4 && lane_id() == kWave - 1) s_wave[w] = incl;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int k = 0; k < min(w, 4); ++k) before += s_wave[k];
+    return before + incl - v;
+}
+
+// Item j of a thread is entry (wave * items + j) * 64 + lane of the tile.
+__device__ __forceinline__ int tile_entry(int items, int j) {
+    return (wave_in_block() * items + j) * kWave + lane_id();
+}
+
+// The place of each item in the tile by its digit, items of one digit in order.
+__device__ __forceinline__ void rank_tile(SortLds &S, const uint32_t *k, int items, int count,
+                                          int shift, int nb, uint32_t *pos) {
+    const int t = threadIdx.x, w = wave_in_block(), radix = 1 << nb;
+    for (int i = t; i < (int)sizeof(S.cnt) / 4; i += kSortBlock)
+        reinterpret_cast<uint32_t *>(S.cnt)[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j) {
+        if (j >= items) continue;
+        const bool valid = tile_entry(items, j) < count;
+        const uint32_t dg = digit_of(k[j], shift, nb);
+        const unsigned long long peers = digit_peers(dg, valid);
+        const unsigned r = lanes_below(peers);
+        // of the wave's items before this one (a wave's LDS accesses run in order)
+        const uint32_t before =
+            __hip_atomic_load(&S.cnt[w][dg], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+        __builtin_amdgcn_wave_barrier();
+        if (valid && r == 0)
+            __hip_atomic_store(&S.cnt[w][dg], before + (uint32_t)__popcll(peers), __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_WAVEFRONT);
+        __builtin_amdgcn_wave_barrier();
+        pos[j] = before + r;
+    }
+    __syncthreads();
+    uint32_t sum = 0;
+    if (t < radix) {
+#pragma unroll
+        for (int q = 0; q < kSortBlock / kWave; ++q) {
+            const uint32_t c = S.cnt[q][t];
+            S.cnt[q][t] = sum;
+            sum += c;
+        }
+    }
+    const uint32_t start = scan256(sum, S.wave);
+    if (t < 256) S.start[t] = start;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j) {
+        if (j >= items) continue;
+        const uint32_t dg = digit_of(k[j], shift, nb);
+        pos[j] += S.start[dg] + S.cnt[w][dg];
+    }
+}
+
+// a token as a sort key: padding goes behind every row of the table
+__device__ __forceinline__ uint32_t token_key(const void *tokens, int index, int64_t i, int64_t v,
+                                              int32_t *status) {
+    const int32_t t = read_token(tokens, index, i, v, status);
+    return t < 0 ? (uint32_t)v : (uint32_t)t;
+}
+
+// Up to kRankTokens tokens: a token's place is the number of those that go before
+// it, counted.  n^2 comparisons of two instructions each, all compute units at
+// it, cost less than the launches of a radix sort.  A block has all keys in LDS and
+// 64 tokens to place, each wave every 16th 64 of the keys.
+constexpr int kRankTokens = 12288;
+__global__ __launch_bounds__(kSortBlock) void k_token_rank(const void *__restrict__ tokens,
+                                                           int index, int n, int64_t v,
+                                                           uint32_t *__restrict__ keys,
+                                                           uint32_t *__restrict__ vals,
+                                                           int32_t *status) {
+    __shared__ __align__(16) uint32_t s_key[kRankTokens];
+    __shared__ uint32_t s_before[kWave];
+    const int blocks = (n + kWave - 1) / kWave, mine = blockIdx.x;
+    for (int i = threadIdx.x; i < blocks * kWave; i += kSortBlock)
+        s_key[i] = i < n ? token_key(tokens, index, i, v, status) : 0xFFFFFFFFu;  // before none
+    if (threadIdx.x < kWave) s_before[threadIdx.x] = 0;
+    __syncthreads();
+    const int lane = lane_id();
+    const uint32_t own = s_key[mine * kWave + lane];
+    uint32_t before = 0;
+    for (int q = wave_in_block(); q < blocks; q += kSortBlock / kWave) {
+        const uint4 *k = reinterpret_cast<const uint4 *>(s_key + q * kWave);
+        if (q == mine) {  // equal ones among these 64: by position
+            for (int j = 0; j < kWave; ++j) {
+                const uint32_t o = s_key[q * kWave + j];
+                before += o < own || (o == own && j < lane);
+            }
+        } else {
+            // an equal one counts where it stands before
+            const uint32_t most = q < mine ? own + 1 : own;
+#pragma unroll
+            for (int j = 0; j < kWave / 4; ++j) {
+                const uint4 o = k[j];
+                before += o.x < most;
+                before += o.y < most;
+                before += o.z < most;
+                before += o.w < most;
+            }
+        }
+    }
+    atomicAdd(&s_before[lane], before);
+    __syncthreads();
+    const int i = mine * kWave + (int)threadIdx.x;
+    if (threadIdx.x < kWave && i < n) {
+        keys[s_before[threadIdx.x]] = own;
+        vals[s_before[threadIdx.x]] = (uint32_t)i;
+    }
+}
+
+// Digit counts of each tile, [tile][digit].  FIRST reads the tokens and leaves
+// their keys.
+template <bool FIRST>
+__global__ __launch_bounds__(kSortBlock) void k_token_sort_count(
+    const void *__restrict__ tokens, int index, int64_t v, int32_t *status,
+    uint32_t *__restrict__ keys, int64_t n, int items, int shift, int nb,
+    uint32_t *__restrict__ hist) {
+    constexpr int kCopies = 4;  // of the counts, for a quarter of the waves each
+    __shared__ uint32_t s_cnt[kCopies][256];
+    const int t = threadIdx.x;
+    uint32_t *mine = s_cnt[wave_in_block() % kCopies];
+    (&s_cnt[0][0])[t] = 0;
+    static_assert(kCopies * 256 == kSortBlock, "one count a thread");
+    __syncthreads();
+    const int64_t base = (int64_t)blockIdx.x * items * kSortBlock;
+    for (int j = 0; j < items; ++j) {
+        const int64_t i = base + j * kSortBlock + t;
+        const bool valid = i < n;
+        uint32_t key = 0;
+        if (FIRST) {
+            if (valid) keys[i] = key = token_key(tokens, index, i, v, status);
+        } else {
+            if (valid) key = keys[i];
+        }
+        const uint32_t dg = digit_of(key, shift, nb);
+        // a digit that many lanes hold is counted once for all of them: adds to one
+        // LDS address go one after another
+        const uint32_t d0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)dg);
+        const unsigned long long same = __ballot(valid && dg == d0);
+        const bool hot = __popcll(same) >= 4;
+        if (hot && lane_id() == 0) atomicAdd(&mine[d0], (uint32_t)__popcll(same));
+        if (valid && !(hot && dg == d0)) atomicAdd(&mine[dg], 1u);
+    }
+    __syncthreads();
+    if (t < (1 << nb)) {
+        uint32_t all = 0;
+#pragma unroll
+        for (int q = 0; q < kCopies; ++q) all += s_cnt[q][t];
+        hist[((int64_t)blockIdx.x << nb) + t] = all;
+    }
+}
+
+// One pass: vals_in NULL means value = position.
+__global__ __launch_bounds__(kSortBlock) void k_token_sort_move(
+    const uint32_t *__restrict__ keys_in, const uint32_t *__restrict__ vals_in, int64_t n, int items,
+    int shift, int nb, const uint32_t *__restrict__ hist, int tiles, uint32_t *__restrict__ keys,
+    uint32_t *__restrict__ vals) {
+    __shared__ SortLds S;
+    const int t = threadIdx.x, radix = 1 << nb;
+    const int64_t base = (int64_t)blockIdx.x * items * kSortBlock;
+    const int count = (int)min((int64_t)items * kSortBlock, n - base);
+    uint32_t k[kSortItems], p[kSortItems], pos[kSortItems];
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j) {
+        if (j >= items) continue;
+        const int e = tile_entry(items, j);
+        k[j] = e < count ? keys_in[base + e] : 0;
+        p[j] = e < count ? (vals_in ? vals_in[base + e] : (uint32_t)(base + e)) : 0;
+    }
+    // where each digit of this tile goes: every smaller digit, and this one in
+    // the tiles before
+    if (t < 256) S.all[t] = S.out[t] = 0;
+    __syncthreads();
+    uint32_t all = 0, before = 0;
+#pragma unroll 8
+    for (int q = t >> nb; q < tiles; q += kSortBlock >> nb) {
+        const uint32_t c = hist[((int64_t)q << nb) + (t & (radix - 1))];
+        all += c;
+        before += q < (int)blockIdx.x ? c : 0;
+    }
+    atomicAdd(&S.all[t & (radix - 1)], all);
+    atomicAdd(&S.out[t & (radix - 1)], before);
+    __syncthreads();
+    const uint32_t smaller = scan256(t < radix ? S.all[t] : 0, S.wave);
+    if (t < radix) S.out[t] += smaller;
+    __syncthreads();
+    rank_tile(S, k, items, count, shift, nb, pos);
+#pragma unroll
+    for (int j = 0; j < kSortItems; ++j) {
+        if (j >= items) continue;
+        if (tile_entry(items, j) < count) {
+            S.key[pos[j]] = k[j];
+            S.val[pos[j]] = p[j];
+        }
+    }
+    __syncthreads();
+    // in the tile's order: consecutive threads write a digit's consecutive slots
+    for (int e = t; e < count; e += kSortBlock) {
+        const uint32_t kk = S.key[e], dg = digit_of(kk, shift, nb);
+        const uint32_t to = S.out[dg] + ((uint32_t)e - S.start[dg]);
+        keys[to] = kk;
+        vals[to] = S.val[e];
+    }
+}
+
+// tokens to sort keys, for the library's sort
+__global__ __launch_bounds__(kBlock) void k_token_keys(const void *__restrict__ tokens, int index,
                                                        int64_t n, int64_t v,
                                                        uint32_t *__restrict__ keys,
                                                        int32_t *status) {
     for (int64_t i = blockIdx.x * (int64_t)kBlock + threadIdx.x; i < n;
-         i += (int64_t)gridDim.x * kBlock) {
-        const int32_t t = read_token(tokens, index, i, v, status);
-        keys[i] = t < 0 ? (uint32_t)v : (uint32_t)t;
-    }
+         i += (int64_t)gridDim.x * kBlock)
+        keys[i] = token_key(tokens, index, i, v, status);
 }
 
-// grad[t] at columns c.. from a finished sum
+// ----------------------------------------------------------------------------
+// gradient: sums
+
+// E elements at column c of a row, as they are stored
+template <int DT, int E>
+struct RawCols {
+    u32x4 r[E / Elem<DT>::kVec];
+};
+template <int DT, int E>
+__device__ __forceinline__ RawCols<DT, E> load_raw(const void *p, int64_t row, int64_t c,
+                                                   int64_t d) {
+    constexpr int kV = Elem<DT>::kVec;
+    RawCols<DT, E> x;
+    if (c + E <= d) {
+#pragma unroll
+        for (int k = 0; k < E / kV; ++k) x.r[k] = load16(elem_at<DT>(p, row + c + k * kV));
+    } else {
+        float f[E];
+        load_cols<DT, E>(p, row, c, d, f);
+#pragma unroll
+        for (int k = 0; k < E / kV; ++k) x.r[k] = pack<DT>(f + k * kV);
+    }
+    return x;
+}
+template <int DT, int E>
+__device__ __forceinline__ void unpack_raw(const RawCols<DT, E> &x, float *f) {
+    constexpr int kV = Elem<DT>::kVec;
+#pragma unroll
+    for (int k = 0; k < E / kV; ++k) unpack<DT>(x.r[k], f + k * kV);
+}
+
+// grad[t] at columns c.. from a finished sum and what it held (accumulate)
 template <int GT, int E>
 __device__ __forceinline__ void put_row(void *grad, int64_t ldg, uint32_t t, int64_t c, int64_t d,
-                                        float scale, bool accumulate, const float *sum) {
+                                        float scale, bool accumulate, const RawCols<GT, E> &old,
+                                        const float *sum) {
     float x[E];
     if (accumulate) {
-        load_cols<GT, E>(grad, (int64_t)t * ldg, c, d, x);
+        unpack_raw<GT, E>(old, x);
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = __builtin_fmaf(scale, sum[e], x[e]);
     } else {
@@ -117,62 +399,39 @@ __device__ __forceinline__ void put_row(void *grad, int64_t ldg, uint32_t t, int
     store_cols<GT, E>(grad, (int64_t)t * ldg, c, d, x);
 }
 
-constexpr int kAhead = 4;  // rows a lane has in flight
-
-// One tile of R sorted entries per group.  part: [tiles][2][d], slot 0 what the
-// tile adds to a token that began before it, slot 1 to one that goes on after it.
-template <int DT, int GT>
-__global__ __launch_bounds__(kBlock) void k_embed_tiles(
-    const void *__restrict__ dy, int64_t ldy, const uint32_t *__restrict__ keys,
-    const uint32_t *__restrict__ vals, int64_t n, int64_t d, int64_t v, int R, int lg, float scale,
-    int accumulate, void *__restrict__ grad, int64_t ldg, float *__restrict__ part) {
-    constexpr int kE = Pair<DT, GT>::kE;
+// zeros in those of the 64 rows from r0 on that `free` names
+template <int GT>
+__device__ __forceinline__ void zero_rows(void *grad, int64_t ldg, int64_t r0, int64_t d, int lg,
+                                          unsigned long long free) {
+    constexpr int kE = Elem<GT>::kVec;
+    const float zero[kE] = {};
     const int lane = threadIdx.x & ((1 << lg) - 1);
-    const int64_t tile = (int64_t)blockIdx.x * (kBlock >> lg) + (threadIdx.x >> lg);
-    const int64_t c = ((int64_t)blockIdx.y << lg | lane) * kE;
-    const int64_t e0 = tile * R, e1 = min(n, e0 + R);
-    if (e0 >= n || c >= d) return;
-    float sum[kE];
-#pragma unroll
-    for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
-    uint32_t cur = keys[e0];
-    bool began = e0 > 0 && keys[e0 - 1] == cur;  // cur's first entry lies in an earlier tile
-    for (int64_t e = e0; e < e1; e += kAhead) {
-        uint32_t t[kAhead];
-        float x[kAhead][kE];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int64_t at = min(e + k, e1 - 1);
-            t[k] = keys[at];
-            if (t[k] < (uint32_t)v) load_cols<DT, kE>(dy, (int64_t)vals[at] * ldy, c, d, x[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (e + k >= e1 || cur == (uint32_t)v) break;  // padding comes last
-            if (t[k] != cur) {
-                if (began)
-                    store_cols<PDB_F32, kE>(part, (tile * 2) * d, c, d, sum);
-                else
-                    put_row<GT, kE>(grad, ldg, cur, c, d, scale, accumulate, sum);
-                began = false;
-                cur = t[k];
-                if (cur == (uint32_t)v) break;
-#pragma unroll
-                for (int q = 0; q < kE; ++q) sum[q] = 0.0f;
-            }
-#pragma unroll
-            for (int q = 0; q < kE; ++q) sum[q] += x[k][q];
-        }
-    }
-    if (cur == (uint32_t)v) return;
-    const bool goes_on = e1 < n && keys[e1] == cur;
-    if (began)
-        store_cols<PDB_F32, kE>(part, (tile * 2) * d, c, d, sum);
-    else if (goes_on)
-        store_cols<PDB_F32, kE>(part, (tile * 2 + 1) * d, c, d, sum);
-    else
-        put_row<GT, kE>(grad, ldg, cur, c, d, scale, accumulate, sum);
+    for (int q = threadIdx.x >> lg; q < kWave; q += kBlock >> lg)
+        if ((free >> q) & 1ull)
+            for (int64_t c = (int64_t)lane * kE; c < d; c += (int64_t)kE << lg)
+                store_cols<GT, kE>(grad, (r0 + q) * ldg, c, d, zero);
 }
+
+constexpr int kAhead = 4;         // rows a lane has in flight
+constexpr int kStaged = 1024;     // entries of a block's tiles, in LDS
+constexpr int kDirect = kBlock;   // tokens that the direct kernel takes
+
+struct GradArgs {
+    const void *dy;
+    int64_t ldy;
+    const uint32_t *keys, *vals;  // sorted
+    const void *tokens;           // the direct kernel's
+    int index;
+    int64_t n, d, v;
+    int R, lg, zero_lg;    // entries of a tile; lanes of a row (log2)
+    int64_t span;          // entries of a block's tiles
+    int64_t sum_blocks, zero_blocks;
+    float scale;
+    void *grad;
+    int64_t ldg;
+    float *part;  // [sum_blocks][2][d]
+    int32_t *status;
+};
 
 // first entry whose key is >= t
 __device__ __forceinline__ int64_t lower_bound_key(const uint32_t *keys, int64_t lo, int64_t hi,
@@ -187,120 +446,309 @@ __device__ __forceinline__ int64_t lower_bound_key(const uint32_t *keys, int64_t
     return lo;
 }
 
-// Tokens that cross tiles: the group of the tile where one begins adds the
-// later tiles' slots to its own, in tile order.  A run of more than kOwn tiles is
-// added by the whole block: every group takes each G-th tile, then the groups'
-// sums are added in order.
-constexpr int kOwn = 16;
-template <int GT, int E>
-__global__ __launch_bounds__(kBlock) void k_embed_join(const uint32_t *__restrict__ keys, int64_t n,
-                                                       int64_t d, int64_t v, int64_t tiles, int R,
-                                                       int lg, float scale, int accumulate,
-                                                       void *__restrict__ grad, int64_t ldg,
-                                                       const float *__restrict__ part) {
-    __shared__ float s_sum[kBlock * E];
-    __shared__ int64_t s_last[kBlock];
-    const int L = 1 << lg, lane = threadIdx.x & (L - 1);
-    const int groups = kBlock >> lg, g = threadIdx.x >> lg;
-    const int64_t tile0 = (int64_t)blockIdx.x * groups;
-    const int64_t c = ((int64_t)blockIdx.y << lg | lane) * E;
-    auto add_slots = [&](float *sum, int64_t from, int64_t to, int64_t step) {
-        for (int64_t q = from; q <= to; q += step * kAhead) {
-            float x[kAhead][E];
+// The blocks that sum and those that write zeros alternate: the first wait for
+// scattered rows, the second for nothing.  -1: nothing to do.
+__device__ __forceinline__ int64_t sum_block(const GradArgs &p, int64_t x, bool &zero) {
+    const int64_t both = 2 * min(p.sum_blocks, p.zero_blocks);
+    zero = x < both ? x & 1 : p.zero_blocks > p.sum_blocks;
+    return x < both ? x >> 1 : x - (both >> 1);
+}
+
+// One tile of R sorted entries per group, a block's tiles one after another.  A
+// token that lies in one tile is written by its group.  One that crosses tiles of
+// the block is joined in LDS by the group where it begins.  One that crosses blocks
+// goes to the partials: slot 0 of a block is what it adds to a token that began
+// before it, slot 1 to one that goes on after it.
+template <int DT, int GT, bool ACC>
+__global__ __launch_bounds__(kBlock) void k_embed_tiles(GradArgs p) {
+    constexpr int kE = Pair<DT, GT>::kE;
+    __shared__ uint32_t s_key[kStaged + 2], s_val[kStaged];
+    __shared__ float s_head[kBlock * kE];  // of each group, what it adds to a token from before it
+    __shared__ unsigned long long s_free;
+    bool zero;
+    const int64_t block = sum_block(p, blockIdx.x, zero);
+    if (!ACC && zero) {
+        if (blockIdx.y > 0) return;
+        for (int64_t r0 = block * kWave; r0 < p.v; r0 += p.zero_blocks * kWave) {
+            if (wave_in_block() == 0) {
+                const int64_t r = r0 + lane_id();
+                bool free = false;
+                if (r < p.v) {
+                    const int64_t at = lower_bound_key(p.keys, 0, p.n, (uint32_t)r);
+                    free = at >= p.n || p.keys[at] != (uint32_t)r;
+                }
+                const unsigned long long m = __ballot(free);
+                if (lane_id() == 0) s_free = m;
+            }
+            __syncthreads();
+            zero_rows<GT>(p.grad, p.ldg, r0, p.d, p.zero_lg, s_free);
+            __syncthreads();
+        }
+        return;
+    }
+    const int groups = kBlock >> p.lg, g = threadIdx.x >> p.lg;
+    const int lane = threadIdx.x & ((1 << p.lg) - 1);
+    const int64_t from = block * p.span;
+    // the block's entries, and the key on either side of them (none: 2^32 - 1,
+    // which is no row's)
+    const int here = (int)min(p.span, p.n - from);
+    for (int i = threadIdx.x; i < here + 2; i += kBlock) {
+        const int64_t e = from + i - 1;
+        s_key[i] = e >= 0 && e < p.n ? p.keys[e] : 0xFFFFFFFFu;
+        if (i < here) s_val[i] = p.vals[from + i];
+    }
+    __syncthreads();
+    const int64_t c = ((int64_t)blockIdx.y << p.lg | lane) * kE;
+    const int e0 = g * p.R, e1 = min(here, e0 + p.R);
+    const bool live = e0 < here && c < p.d;
+    const uint32_t none = (uint32_t)p.v;  // padding, which comes last
+    float sum[kE];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (q + k * step <= to)
-                    load_cols<PDB_F32, E>(part, (q + k * step) * 2 * d, c, d, x[k]);
+    for (int q = 0; q < kE; ++q) sum[q] = 0.0f;
+    // whether the tile's first token began before it
+    const bool opened = live && s_key[e0] == s_key[e0 + 1] && s_key[e0] != none;
+    bool began = opened;
+    auto put_head = [&]() {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                if (q + k * step > to) break;
+        for (int q = 0; q < kE; ++q) s_head[q * kBlock + threadIdx.x] = sum[q];
+    };
+    for (int e = e0; live && e < e1; e += kAhead) {
+        RawCols<DT, kE> x[kAhead];
+        RawCols<GT, kE> old[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = min(e + k, e1 - 1);
+            const uint32_t t = s_key[at + 1];
+            if (t == none) break;
+            x[k] = load_raw<DT, kE>(p.dy, (int64_t)s_val[at] * p.ldy, c, p.d);
+            if (ACC && s_key[at + 2] != t)
+                old[k] = load_raw<GT, kE>(p.grad, (int64_t)t * p.ldg, c, p.d);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (e + k >= e1) break;
+            const uint32_t t = s_key[e + k + 1];
+            if (t == none) break;
+            float f[kE];
+            unpack_raw<DT, kE>(x[k], f);
+#pragma unroll
+            for (int q = 0; q < kE; ++q) sum[q] += f[q];
+            if (s_key[e + k + 2] == t) continue;
+            if (began)
+                put_head();
+            else
+                put_row<GT, kE>(p.grad, p.ldg, t, c, p.d, p.scale, ACC, old[k], sum);
+            began = false;
+#pragma unroll
+            for (int q = 0; q < kE; ++q) sum[q] = 0.0f;
+        }
+    }
+    const uint32_t last = live ? s_key[e1] : none;
+    const bool goes_on = last != none && s_key[e1 + 1] == last;
+    if (goes_on && began) put_head();
+    __syncthreads();
+    // what the later tiles of the block add to token t, from group q on
+    auto add_heads = [&](uint32_t t, int q) {
+        for (; q < groups && q * p.R < here && s_key[q * p.R + 1] == t; ++q)
+#pragma unroll
+            for (int k = 0; k < kE; ++k)
+                sum[k] += s_head[k * kBlock + (q << p.lg) + lane];
+    };
+    if (goes_on && !began) {  // it began in this tile
+        add_heads(last, g + 1);
+        if (s_key[here + 1] == last) {
+            store_cols<PDB_F32, kE>(p.part, (block * 2 + 1) * p.d, c, p.d, sum);
+        } else {
+            RawCols<GT, kE> old;
+            if (ACC) old = load_raw<GT, kE>(p.grad, (int64_t)last * p.ldg, c, p.d);
+            put_row<GT, kE>(p.grad, p.ldg, last, c, p.d, p.scale, ACC, old, sum);
+        }
+    }
+    if (g == 0 && opened) {
+#pragma unroll
+        for (int q = 0; q < kE; ++q) sum[q] = 0.0f;
+        add_heads(s_key[0], 0);
+        store_cols<PDB_F32, kE>(p.part, block * 2 * p.d, c, p.d, sum);
+    }
+}
+
+// Tokens that cross the summing blocks' spans: the group of the span where one
+// begins adds the later spans' slots to its own, in order, as long as a span's first
+// entry holds the token (slots and first entries are read together: waiting for one
+// to know whether to read the other would double the trips).  A run of more than
+// kOwn spans is added by the whole block, every group each G-th span and then the
+// groups' sums pairwise.  Groups are narrow, 16 lanes at most, so that a hot
+// token's run is spread over many of them.
+constexpr int kOwn = 16, kJoinBlock = 1024, kJoinLg = 4;
+template <int GT, int E, bool ACC>
+__global__ __launch_bounds__(kJoinBlock) void k_embed_join(GradArgs p) {
+    constexpr int kJoinAhead = 32 / E;  // slots in flight
+    __shared__ float s_sum[kJoinBlock * E / 2];
+    // the groups whose tokens' runs are long, and those tokens
+    __shared__ int s_long[kJoinBlock];
+    __shared__ uint32_t s_token[kJoinBlock];
+    __shared__ int s_count;
+    const int lane = threadIdx.x & ((1 << p.lg) - 1);
+    const int groups = kJoinBlock >> p.lg, g = threadIdx.x >> p.lg;
+    const int64_t span0 = (int64_t)blockIdx.x * groups, span = span0 + g;
+    const int64_t c = ((int64_t)blockIdx.y << p.lg | lane) * E;
+    const bool live = c < p.d;
+    // adds slot 0 of the spans from, from + step, ... below `to`, as long as they
+    // begin with t
+    auto add_slots = [&](float *sum, uint32_t t, int64_t from, int64_t to, int64_t step) {
+        to = min(to, p.sum_blocks);
+        for (int64_t q = from; q < to; q += step * kJoinAhead) {
+            uint32_t key[kJoinAhead];
+            float x[kJoinAhead][E];
+#pragma unroll
+            for (int k = 0; k < kJoinAhead; ++k) {
+                const int64_t at = min(q + k * step, p.sum_blocks - 1);
+                key[k] = p.keys[at * p.span];
+                load_cols<PDB_F32, E>(p.part, at * 2 * p.d, c, p.d, x[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < kJoinAhead; ++k) {
+                if (q + k * step >= to || key[k] != t) return;
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] += x[k][e];
             }
         }
     };
-    // the last tile of the token that begins in this group's tile and goes on; -1 none
-    const int64_t tile = tile0 + g;
-    int64_t last = -1;
-    uint32_t t = 0;
-    if (tile < tiles - 1) {
-        const int64_t e0 = tile * R, e1 = e0 + R;
-        t = keys[e1 - 1];
-        const bool whole = e0 > 0 && keys[e0 - 1] == t;  // it began before this tile
-        if (t < (uint32_t)v && keys[e1] == t && !whole)
-            last = (lower_bound_key(keys, e1, n, t + 1) - 1) / R;
-    }
-    const bool mine = last >= 0 && last - tile <= kOwn;
-    if (mine && c < d) {
-        float sum[E];
-        load_cols<PDB_F32, E>(part, (tile * 2 + 1) * d, c, d, sum);
-        add_slots(sum, tile + 1, last, 1);
-        put_row<GT, E>(grad, ldg, t, c, d, scale, accumulate, sum);
-    }
-    if (lane == 0) s_last[g] = last >= 0 && !mine ? last : -1;
+    if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
-    for (int k = 0; k < groups; ++k) {
-        const int64_t to = s_last[k];
-        if (to < 0) continue;
-        const int64_t from = tile0 + k;
+    if (span < p.sum_blocks - 1) {
+        const int64_t e0 = span * p.span, e1 = e0 + p.span, far = span + 1 + kOwn;
+        const uint32_t t = p.keys[e1 - 1], next = p.keys[e1];
+        const uint32_t before = e0 > 0 ? p.keys[e0 - 1] : 0xFFFFFFFFu;
+        const uint32_t there = far < p.sum_blocks ? p.keys[far * p.span] : 0xFFFFFFFFu;
+        // it goes on, and began in this span
+        if (t < (uint32_t)p.v && next == t && before != t) {
+            if (there == t) {
+                if (lane == 0) {
+                    const int k = atomicAdd(&s_count, 1);
+                    s_long[k] = g;
+                    s_token[k] = t;
+                }
+            } else if (live) {
+                RawCols<GT, E> old;
+                if (ACC) old = load_raw<GT, E>(p.grad, (int64_t)t * p.ldg, c, p.d);
+                float sum[E];
+                load_cols<PDB_F32, E>(p.part, (span * 2 + 1) * p.d, c, p.d, sum);
+                add_slots(sum, t, span + 1, far, 1);
+                put_row<GT, E>(p.grad, p.ldg, t, c, p.d, p.scale, ACC, old, sum);
+            }
+        }
+    }
+    __syncthreads();
+    const int count = s_count;
+    for (int k = 0; k < count; ++k) {
+        const int64_t from = span0 + s_long[k];
+        const uint32_t t = s_token[k];
+        RawCols<GT, E> old;
+        if (ACC && g == 0 && live) old = load_raw<GT, E>(p.grad, (int64_t)t * p.ldg, c, p.d);
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-        if (c < d) {
-            if (g == 0) load_cols<PDB_F32, E>(part, (from * 2 + 1) * d, c, d, sum);
-            add_slots(sum, from + 1 + g, to, groups);
+        if (live) {
+            if (g == 0) load_cols<PDB_F32, E>(p.part, (from * 2 + 1) * p.d, c, p.d, sum);
+            add_slots(sum, t, from + 1 + g, p.sum_blocks, groups);
         }
+        for (int half = groups >> 1; half >= 1; half >>= 1) {
+            if (g >= half && g < 2 * half)
 #pragma unroll
-        for (int e = 0; e < E; ++e) s_sum[threadIdx.x * E + e] = sum[e];
-        __syncthreads();
-        if (g == 0 && c < d) {
-            for (int q = 1; q < groups; ++q)
+                for (int e = 0; e < E; ++e)
+                    s_sum[e * (kJoinBlock / 2) + threadIdx.x - (half << p.lg)] = sum[e];
+            __syncthreads();
+            if (g < half)
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] += s_sum[(q * L + lane) * E + e];
-            put_row<GT, E>(grad, ldg, keys[from * R + R - 1], c, d, scale, accumulate, sum);
+                for (int e = 0; e < E; ++e) sum[e] += s_sum[e * (kJoinBlock / 2) + threadIdx.x];
+            __syncthreads();
         }
-        __syncthreads();
+        if (g == 0 && live)
+            put_row<GT, E>(p.grad, p.ldg, t, c, p.d, p.scale, ACC, old, sum);
     }
 }
 
-// zeros in the rows of the table that no token picked, 64 rows per block
-template <int GT>
-__global__ __launch_bounds__(kBlock) void k_embed_zero(const uint32_t *__restrict__ keys, int64_t n,
-                                                       int64_t d, int64_t v, int lg,
-                                                       void *__restrict__ grad, int64_t ldg) {
-    constexpr int kE = Elem<GT>::kVec;
-    __shared__ unsigned long long s_free;
-    const float zero[kE] = {};
-    const int lane = threadIdx.x & ((1 << lg) - 1);
-    for (int64_t r0 = (int64_t)blockIdx.x * kWave; r0 < v; r0 += (int64_t)gridDim.x * kWave) {
-        if (wave_in_block() == 0) {
-            const int64_t r = r0 + lane_id();
-            bool free = false;
-            if (r < v) {
-                const int64_t at = lower_bound_key(keys, 0, n, (uint32_t)r);
-                free = at >= n || keys[at] != (uint32_t)r;
+// Few tokens: no sort.  A group per token; the first of equal ones sums them all.
+template <int DT, int GT, bool ACC>
+__global__ __launch_bounds__(kBlock) void k_embed_direct(GradArgs p) {
+    constexpr int kE = Pair<DT, GT>::kE;
+    __shared__ int32_t s_tok[kDirect];
+    __shared__ unsigned long long s_used;
+    const int n = (int)p.n;
+    if (threadIdx.x < n) s_tok[threadIdx.x] = read_token(p.tokens, p.index, threadIdx.x, p.v, p.status);
+    __syncthreads();
+    if ((int64_t)blockIdx.x >= p.sum_blocks) {  // zeros in the rows without tokens
+        if (blockIdx.y > 0) return;
+        for (int64_t r0 = ((int64_t)blockIdx.x - p.sum_blocks) * kWave; r0 < p.v;
+             r0 += p.zero_blocks * kWave) {
+            if (threadIdx.x == 0) s_used = 0;
+            __syncthreads();
+            if (threadIdx.x < n) {
+                const int64_t at = s_tok[threadIdx.x] - r0;
+                if (s_tok[threadIdx.x] >= 0 && at >= 0 && at < kWave)
+                    atomicOr(&s_used, 1ull << at);
             }
-            const unsigned long long m = __ballot(free);
-            if (lane_id() == 0) s_free = m;
+            __syncthreads();
+            const int64_t rows = p.v - r0;
+            const unsigned long long there = rows >= kWave ? ~0ull : (1ull << rows) - 1ull;
+            zero_rows<GT>(p.grad, p.ldg, r0, p.d, p.zero_lg, there & ~s_used);
+            __syncthreads();
         }
-        __syncthreads();
-        const unsigned long long m = s_free;
-        for (int q = threadIdx.x >> lg; q < kWave; q += kBlock >> lg)
-            if ((m >> q) & 1ull)
-                for (int64_t c = (int64_t)lane * kE; c < d; c += (int64_t)kE << lg)
-                    store_cols<GT, kE>(grad, (r0 + q) * ldg, c, d, zero);
-        __syncthreads();
+        return;
     }
+    // a group's part of its wave, and the tokens compared at a time
+    const int lw = min(p.lg, 6), step = 1 << lw;
+    const int lane = threadIdx.x & ((1 << p.lg) - 1), in_wave = lane_id() & (step - 1);
+    const int first = lane_id() & ~(step - 1);
+    const int i = (int)blockIdx.x * (kBlock >> p.lg) + (threadIdx.x >> p.lg);
+    const int64_t c = ((int64_t)blockIdx.y << p.lg | lane) * kE;
+    const int32_t t = i < n ? s_tok[i] : -1;
+    bool mine = t >= 0;
+    float sum[kE];
+#pragma unroll
+    for (int q = 0; q < kE; ++q) sum[q] = 0.0f;
+    RawCols<GT, kE> old;
+    if (ACC && mine && c < p.d) old = load_raw<GT, kE>(p.grad, (int64_t)t * p.ldg, c, p.d);
+    for (int j0 = 0; j0 < n; j0 += step) {
+        const bool same = mine && j0 + in_wave < n && s_tok[j0 + in_wave] == t;
+        unsigned long long m = __ballot(same) >> first;
+        if (step < 64) m &= (1ull << step) - 1ull;
+        if (mine && m && j0 + (int)__builtin_ctzll(m) < i) mine = false;  // not the first
+        while (mine && m) {
+            RawCols<DT, kE> x[kAhead];
+            int count = 0;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (!m) break;
+                const int j = j0 + (int)__builtin_ctzll(m);
+                m &= m - 1;
+                if (c < p.d) x[k] = load_raw<DT, kE>(p.dy, (int64_t)j * p.ldy, c, p.d);
+                count = k + 1;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (k >= count) break;
+                float f[kE];
+                unpack_raw<DT, kE>(x[k], f);
+#pragma unroll
+                for (int q = 0; q < kE; ++q) sum[q] += f[q];
+            }
+        }
+    }
+    if (mine && c < p.d) put_row<GT, kE>(p.grad, p.ldg, (uint32_t)t, c, p.d, p.scale, ACC, old, sum);
 }
 
 // ----------------------------------------------------------------------------
 
 // Entries per tile.  Enough tiles that n d / R elements, about 2^22, fill the
-// card's lanes with one vector each; not fewer than 8, so that few partials are
-// written, nor more than 256.
-inline int tile_rows(int64_t n, int64_t d) {
+// card's lanes with one vector each; not fewer than 8, so that few sums cross tiles,
+// nor more than a block's tiles have room for in LDS.
+inline int tile_rows(int64_t n, int64_t d, int lg) {
+    const int groups = kBlock >> lg;
     const int64_t r = (n * d) >> 22;
-    return (int)std::min<int64_t>(std::max<int64_t>(r, 8), 256);
+    return (int)std::min<int64_t>(std::max<int64_t>(r, groups > kStaged / 8 ? kStaged / groups : 8),
+                                  std::min(256, kStaged / groups));
 }
 
 struct GradWs {
@@ -309,7 +757,9 @@ struct GradWs {
     size_t total;
 };
 GradWs grad_ws_layout(void *base, int64_t n, int64_t d) {
-    GradWs w;
+    GradWs w = {};
+    w.total = (size_t)kAlign;  // never none: callers pass one workspace for any n
+    if (n <= kDirect) return w;
     char *p = static_cast<char *>(base);
     size_t off = 0;
     auto take = [&](int64_t bytes) {
@@ -317,17 +767,108 @@ GradWs grad_ws_layout(void *base, int64_t n, int64_t d) {
         off += (size_t)align_up(bytes);
         return at;
     };
-    const int64_t st = cdiv(std::max<int64_t>(n, 1), kTile), R = tile_rows(n, d);
-    w.keys = reinterpret_cast<uint32_t *>(take(4 * n));
+    const int64_t st = cdiv(n, kTile);
+    // spans of a block's tiles, for the wider of a lane's shares of a row
+    const int lg = lanes_log2(cdiv(std::max<int64_t>(d, 1), 4));
+    const int lg8 = lanes_log2(cdiv(std::max<int64_t>(d, 1), 8));
+    const int64_t spans = std::max(cdiv(n, (int64_t)tile_rows(n, d, lg) << (8 - lg)),
+                                   cdiv(n, (int64_t)tile_rows(n, d, lg8) << (8 - lg8)));
     w.kA = reinterpret_cast<uint32_t *>(take(4 * n));
     w.vA = reinterpret_cast<uint32_t *>(take(4 * n));
-    w.kB = reinterpret_cast<uint32_t *>(take(4 * n));
-    w.vB = reinterpret_cast<uint32_t *>(take(4 * n));
-    w.hist = reinterpret_cast<uint32_t *>(take(4 * 256 * st));
-    w.scan_tmp = reinterpret_cast<uint32_t *>(take(4 * (int64_t)scan_tmp_elems(256 * st)));
-    w.part = reinterpret_cast<float *>(take(cdiv(n, R) * 2 * d * 4));
+    if (n > kRankTokens) {
+        w.keys = reinterpret_cast<uint32_t *>(take(4 * n));
+        w.kB = reinterpret_cast<uint32_t *>(take(4 * n));
+        w.vB = reinterpret_cast<uint32_t *>(take(4 * n));
+        w.hist = reinterpret_cast<uint32_t *>(take(4 * 256 * std::max<int64_t>(st, kSortTiles)));
+        w.scan_tmp = reinterpret_cast<uint32_t *>(take(4 * (int64_t)scan_tmp_elems(256 * st)));
+    }
+    w.part = reinterpret_cast<float *>(take(spans * 2 * d * 4));
     w.total = off;
     return w;
+}
+
+// The tokens in order (padding as v, last) and their positions.
+int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64_t v,
+                int32_t *status, uint32_t **keys, uint32_t **vals, hipStream_t s) {
+    int bits = 1;
+    while (((int64_t)1 << bits) <= v) ++bits;
+    *keys = w.kA;
+    *vals = w.vA;
+    if (n <= kRankTokens) {
+        k_token_rank<<<(unsigned)cdiv(n, kWave), kSortBlock, 0, s>>>(tokens, index, (int)n, v, w.kA,
+                                                                     w.vA, status);
+        PDB_LAUNCHED();
+        return PDB_OK;
+    }
+    if (n > (int64_t)kSortTiles * kSortTile) {
+        k_token_keys<<<grid_for(n, kBlock, 4096), kBlock, 0, s>>>(tokens, index, n, v, w.keys,
+                                                                  status);
+        PDB_LAUNCHED();
+        PDB_HIP(radix_sort_pairs(w.keys, nullptr, n, bits, w.kA, w.vA, w.kB, w.vB, w.hist,
+                                 w.scan_tmp, keys, vals, s));
+        return PDB_OK;
+    }
+    // about 128 tiles: half of the compute units, and counts that are soon summed
+    const int items = (int)std::min<int64_t>(kSortItems, cdiv(n, 128 * kSortBlock));
+    const int tiles = (int)cdiv(n, (int64_t)items * kSortBlock);
+    const int passes = (bits + 7) / 8, step = (bits + passes - 1) / passes;
+    const uint32_t *ck = w.keys, *cv = nullptr;
+    for (int shift = 0; shift < bits; shift += step) {
+        const int nb = std::min(step, bits - shift);
+        if (shift == 0)
+            k_token_sort_count<true><<<tiles, kSortBlock, 0, s>>>(tokens, index, v, status, w.keys,
+                                                                  n, items, shift, nb, w.hist);
+        else
+            k_token_sort_count<false><<<tiles, kSortBlock, 0, s>>>(
+                nullptr, 0, v, nullptr, const_cast<uint32_t *>(ck), n, items, shift, nb, w.hist);
+        PDB_LAUNCHED();
+        uint32_t *tk = ck == w.kA ? w.kB : w.kA, *tv = ck == w.kA ? w.vB : w.vA;
+        k_token_sort_move<<<tiles, kSortBlock, 0, s>>>(ck, cv, n, items, shift, nb, w.hist, tiles,
+                                                       tk, tv);
+        PDB_LAUNCHED();
+        ck = tk;
+        cv = tv;
+        *keys = tk;
+        *vals = tv;
+    }
+    return PDB_OK;
+}
+
+template <int DT, int GT, bool ACC>
+int embed_grad(GradArgs p, const GradWs &w, hipStream_t s) {
+    constexpr int kE = Pair<DT, GT>::kE;
+    const int64_t vectors = cdiv(p.d, kE);
+    p.lg = lanes_log2(vectors);
+    p.zero_lg = lanes_log2(cdiv(p.d, Elem<GT>::kVec));
+    p.zero_blocks = ACC ? 0 : std::min<int64_t>(cdiv(p.v, kWave), 1 << 18);
+    const int64_t slices = cdiv(vectors, 1 << p.lg), per = kBlock >> p.lg;
+    if (cdiv(vectors, 1 << std::min(p.lg, kJoinLg)) > 65535) return PDB_ERR_UNSUPPORTED;
+    if (p.n <= kDirect) {
+        p.sum_blocks = cdiv(p.n, per);
+        const dim3 grid((unsigned)(p.sum_blocks + p.zero_blocks), (unsigned)slices);
+        k_embed_direct<DT, GT, ACC><<<grid, kBlock, 0, s>>>(p);
+        PDB_LAUNCHED();
+        return PDB_OK;
+    }
+    uint32_t *keys, *vals;
+    const int rc = sort_tokens(w, p.tokens, p.index, p.n, p.v, p.status, &keys, &vals, s);
+    if (rc != PDB_OK) return rc;
+    p.keys = keys;
+    p.vals = vals;
+    p.part = w.part;
+    p.R = tile_rows(p.n, p.d, p.lg);
+    p.span = per * p.R;
+    p.sum_blocks = cdiv(p.n, p.span);
+    const dim3 grid((unsigned)(p.sum_blocks + p.zero_blocks), (unsigned)slices);
+    k_embed_tiles<DT, GT, ACC><<<grid, kBlock, 0, s>>>(p);
+    PDB_LAUNCHED();
+    if (p.sum_blocks == 1) return PDB_OK;
+    p.lg = std::min(p.lg, kJoinLg);
+    const dim3 join((unsigned)cdiv(p.sum_blocks, kJoinBlock >> p.lg),
+                    (unsigned)cdiv(vectors, 1 << p.lg));
+    k_embed_join<GT, kE, ACC><<<join, kJoinBlock, 0, s>>>(p);
+    PDB_LAUNCHED();
+    return PDB_OK;
 }
 
 }  // namespace
@@ -376,42 +917,24 @@ extern "C" int pdb_embed_grad(const void *dy, int dtype, int64_t ldy, const void
     if (accumulate != 0 && accumulate != 1) return PDB_ERR_INVALID_ARG;
     if (v == 0 || d == 0 || (n == 0 && accumulate)) return PDB_OK;
     const GradWs w = grad_ws_layout(ws, n, d);
-    if (w.total > 0 && (!ws || ws_bytes < w.total)) return PDB_ERR_WORKSPACE;
-    uint32_t *keys = nullptr, *vals = nullptr;
-    if (n > 0) {
-        k_embed_keys<<<grid_for(n, kBlock, 4096), kBlock, 0, s>>>(tokens, index, n, v, w.keys,
-                                                                  status);
-        PDB_LAUNCHED();
-        int bits = 1;
-        while (((int64_t)1 << bits) <= v) ++bits;
-        PDB_HIP(radix_sort_pairs(w.keys, nullptr, n, bits, w.kA, w.vA, w.kB, w.vB, w.hist,
-                                 w.scan_tmp, &keys, &vals, s));
-    }
-    const int R = tile_rows(n, d);
-    const int64_t tiles = cdiv(n, R);
+    if (!ws || ws_bytes < w.total) return PDB_ERR_WORKSPACE;
+    GradArgs p = {};
+    p.dy = dy;
+    p.ldy = ldy;
+    p.tokens = tokens;
+    p.index = index;
+    p.n = n;
+    p.d = d;
+    p.v = v;
+    p.scale = scale;
+    p.grad = grad;
+    p.ldg = ldg;
+    p.status = status;
     return with_dtype(grad_dtype, [&](auto gt) -> int {
-        constexpr int GT = decltype(gt)::value;
-        if (!accumulate) {
-            const int lg = lanes_log2(cdiv(d, Elem<GT>::kVec));
-            k_embed_zero<GT><<<grid_for(v, kWave, 1 << 16), kBlock, 0, s>>>(keys, n, d, v, lg, grad,
-                                                                            ldg);
-            PDB_LAUNCHED();
-        }
-        if (n == 0) return PDB_OK;
         return with_dtype(dtype, [&](auto dt) -> int {
-            constexpr int DT = decltype(dt)::value, kE = Pair<DT, GT>::kE;
-            const int64_t vectors = cdiv(d, kE);
-            const int lg = lanes_log2(vectors);
-            const int64_t slices = cdiv(vectors, 1 << lg);
-            if (slices > 65535) return PDB_ERR_UNSUPPORTED;
-            const dim3 grid((unsigned)cdiv(tiles, kBlock >> lg), (unsigned)slices);
-            k_embed_tiles<DT, GT><<<grid, kBlock, 0, s>>>(dy, ldy, keys, vals, n, d, v, R, lg, scale,
-                                                          accumulate, grad, ldg, w.part);
-            PDB_LAUNCHED();
-            k_embed_join<GT, kE><<<grid, kBlock, 0, s>>>(keys, n, d, v, tiles, R, lg, scale,
-                                                         accumulate, grad, ldg, w.part);
-            PDB_LAUNCHED();
-            return PDB_OK;
+            constexpr int DT = decltype(dt)::value, GT = decltype(gt)::value;
+            return accumulate ? embed_grad<DT, GT, true>(p, w, s)
+                              : embed_grad<DT, GT, false>(p, w, s);
         });
     });
 }
