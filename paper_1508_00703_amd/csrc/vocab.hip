@@ -650,7 +650,7 @@ extern "C" int pdb_token_logprobs(const void *logits, int dtype, int64_t ldz, in
                                status, cut.vecs, cut.parts, static_cast<float *>(ws),
                                reinterpret_cast<uint32_t *>(
                                    static_cast<char *>(ws) + stat_bytes(std::min(n, kWantBlocks)))};
-        const bool wave = wave_rows(cut, n, v, kV) && top <= TopLds<1>::kTop;
+        const bool wave = wave_rows(cut, n, v, kV, top > 0) && top <= TopLds<1>::kTop;
         const unsigned blocks = blocks_for(n * cut.parts, wave ? Team<1>::kPerBlock : 1);
         if (wave && top > 0)
             k_logprobs<DT, 1, true><<<blocks, kBlock, 0, s>>>(p);
@@ -687,7 +687,7 @@ extern "C" int pdb_token_logprobs_grad(const void *logits, int dtype, int64_t ld
         const Parts cut = cut_rows(n, v, kV, kMostParts);
         const LogprobGradArgs p = {logits, ldz, n, v, tokens, index, 1.0f / temp, stats, entropy,
                                    d_logp, d_entropy, dlogits, ldd, status, cut.vecs, cut.parts};
-        if (wave_rows(cut, n, v, kV))
+        if (wave_rows(cut, n, v, kV, false))
             k_logprobs_grad<DT, 1><<<blocks_for(n, Team<1>::kPerBlock), kBlock, 0, s>>>(p);
         else
             k_logprobs_grad<DT, kBlock / kWave><<<blocks_for(n * cut.parts), kBlock, 0, s>>>(p);

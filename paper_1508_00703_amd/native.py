@@ -8,6 +8,7 @@ there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -581,106 +582,112 @@ _DTYPES = {torch.float32: PDB_F32, torch.float16: PDB_F16, torch.bfloat16: PDB_B
 _INDEXES = {torch.int32: PDB_I32, torch.int64: PDB_I64}
 
 
-def _matrix(t, name):
-    """(address, pdb_dtype, row stride) of a device matrix."""
+def _matrix(t, name, device=None):
+    """(address, pdb_dtype, row stride) of a matrix on the device (None: on any)."""
     dt = _DTYPES.get(t.dtype)
     if dt is None:
         raise TypeError("%s must be float32, float16 or bfloat16" % name)
     if t.dim() != 2:
         raise ValueError("%s must be a matrix" % name)
-    if not t.is_cuda:
-        raise ValueError("expected a device tensor")
+    if t.get_device() != device and (device is not None or not t.is_cuda):
+        raise ValueError("%s must be a tensor on the call's device" % name)
     rows, cols = t.shape
     if cols > 1 and rows > 0 and t.stride(1) != 1:
         raise ValueError("%s must have unit column stride" % name)
-    return t.data_ptr() or None, dt, t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), dt, t.stride(0) if rows > 1 else cols
 
 
-def _vector(t, name, n, dtype=torch.float32):
-    """Address of a contiguous device vector of n elements; None stays None."""
+def _vector(t, name, n, device, dtype=torch.float32):
+    """Address of n contiguous elements on the device; None stays None."""
     if t is None:
         return None
     if t.dtype != dtype:
         raise TypeError("%s must be %s" % (name, str(dtype).replace("torch.", "")))
     if t.numel() != n:
         raise ValueError("%s must hold %d elements" % (name, n))
-    return _ptr(t)
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s must be contiguous and on the other tensors' device" % name)
+    return t.data_ptr()
 
 
-def _tokens(t, n):
+def _tokens(t, n, device=None):
     """(address, pdb_index) of n tokens; (None, PDB_I32) of None."""
     if t is None:
         return None, PDB_I32
     ix = _INDEXES.get(t.dtype)
     if ix is None:
         raise TypeError("tokens must be int32 or int64")
-    if t.numel() != n:
-        raise ValueError("tokens must hold %d elements" % n)
-    return _ptr(t), ix
+    return _vector(t, "tokens", n, device, t.dtype), ix
 
 
-def _status(status):
-    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+def _status(status, device=None):
+    if status is None:
+        return None
+    if status.dtype != torch.int32 or status.numel() < 1:
         raise TypeError("status must be an int32 device tensor")
-    return _ptr(status)
+    return _vector(status, "status", status.numel(), device, torch.int32)
 
 
-class _Call:
-    """The device and stream of a call, and the tensors allocated for it: those
-    are kept from reuse until the stream is done with them, also where it is not
-    the current one."""
-
-    def __init__(self, device, stream, *tensors):
-        for t in tensors:
-            if t is not None and t.device != device:
-                raise ValueError("tensors on different devices")
-        self.device = device
-        self.other = stream
-        self.guard = None
-        if device.index is not None and device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        self.stream = _stream(self.other, self.device)
-        return self
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-    def empty(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.other is not None:
-            t.record_stream(self.other)
-        return t
-
-    def workspace(self, ws, nbytes):
-        return self.empty(max(nbytes, 1), torch.uint8) if ws is None else ws
+def _raw_stream(stream, device):
+    """The handle of the stream, by default the device's current one."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
+def _empty(like, shape, dtype, stream):
+    """A new tensor on like's device, kept from reuse until the stream, where it is
+    not the current one, is done with it."""
+    t = torch.empty(shape, dtype=dtype, device=like.device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _space(ws, nbytes, like, stream):
+    """(address, bytes) of the given workspace or of a new one, and that tensor."""
+    if ws is None:
+        ws = _empty(like, nbytes, torch.uint8, stream)
+    elif ws.get_device() != like.get_device() or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous and on the other tensors' device")
+    return ws.data_ptr(), ws.numel(), ws
+
+
+def _on_own_device(call):
+    """Runs a call with its first tensor's device as the current one."""
+    @functools.wraps(call)
+    def run(first, *args, **kw):
+        if first.is_cuda and first.get_device() != torch._C._cuda_getDevice():
+            with torch.cuda.device(first.device):
+                return call(first, *args, **kw)
+        return call(first, *args, **kw)
+    return run
+
+
+@_on_own_device
 def pdb_embed_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out=None,
                      out_dtype=None, status=None, stream=None) -> torch.Tensor:
     """scale * table[tokens] as a tensor of tokens.shape + (d,); zeros where a
     token is negative.  out: None, or a matrix of tokens.numel() rows to fill."""
     tp, tdt, ld = _matrix(table, "table")
+    dev = table.get_device()
     v, d = table.shape
     n = tokens.numel()
-    kp, ix = _tokens(tokens, n)
-    with _Call(table.device, stream, tokens, out, status) as c:
-        shaped = out
-        if out is None:
-            shaped = c.empty(tuple(tokens.shape) + (d,), out_dtype or table.dtype)
-            out = shaped.view(n, d)
-        elif tuple(out.shape) != (n, d) or (out_dtype or out.dtype) != out.dtype:
+    kp, ix = _tokens(tokens, n, dev)
+    if out is None:
+        out = _empty(table, (*tokens.shape, d), out_dtype or table.dtype, stream)
+        op, odt, ldo = out.data_ptr(), _DTYPES.get(out.dtype), d
+        if odt is None:
+            raise TypeError("out_dtype must be float32, float16 or bfloat16")
+    else:
+        op, odt, ldo = _matrix(out, "out", dev)
+        if tuple(out.shape) != (n, d) or (out_dtype or out.dtype) != out.dtype:
             raise ValueError("out must be %d x %d (of out_dtype, if given)" % (n, d))
-        op, odt, ldo = _matrix(out, "out")
-        _check(load().pdb_embed_lookup(tp, tdt, ld, v, d, kp, ix, n, scale, op, odt, ldo,
-                                       _status(status), c.stream), "pdb_embed_lookup")
-    return shaped
+    _check(load().pdb_embed_lookup(tp, tdt, ld, v, d, kp, ix, n, scale, op, odt, ldo,
+                                   _status(status, dev), _raw_stream(stream, dev)),
+           "pdb_embed_lookup")
+    return out
 
 
+@functools.lru_cache(maxsize=256)
 def pdb_embed_grad_workspace_bytes(n: int, v: int, d: int) -> int:
     out = ctypes.c_size_t(0)
     _check(load().pdb_embed_grad_workspace_bytes(n, v, d, ctypes.byref(out)),
@@ -688,6 +695,7 @@ def pdb_embed_grad_workspace_bytes(n: int, v: int, d: int) -> int:
     return out.value
 
 
+@_on_own_device
 def pdb_embed_grad(dy: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,
                    accumulate: bool = False, ws=None, status=None, stream=None) -> torch.Tensor:
     """grad[t] = scale * the sum of dy's rows of token t, zeros elsewhere; with
@@ -695,18 +703,18 @@ def pdb_embed_grad(dy: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, s
     SGD step on the rows in use).  dy: tokens.shape + (d,), or its matrix."""
     n = tokens.numel()
     gp, gdt, ldg = _matrix(grad, "grad")
+    dev = grad.get_device()
     v, d = grad.shape
     if dy.dim() != 2:
         dy = dy.view(n, d)
-    yp, ydt, ldy = _matrix(dy, "dy")
+    yp, ydt, ldy = _matrix(dy, "dy", dev)
     if tuple(dy.shape) != (n, d):
         raise ValueError("dy must be %d x %d" % (n, d))
-    kp, ix = _tokens(tokens, n)
-    with _Call(grad.device, stream, dy, tokens, ws, status) as c:
-        ws = c.workspace(ws, pdb_embed_grad_workspace_bytes(n, v, d))
-        _check(load().pdb_embed_grad(yp, ydt, ldy, kp, ix, n, gp, gdt, ldg, v, d, scale,
-                                     1 if accumulate else 0, _status(status), _ptr(ws), ws.numel(),
-                                     c.stream), "pdb_embed_grad")
+    kp, ix = _tokens(tokens, n, dev)
+    wp, size, ws = _space(ws, pdb_embed_grad_workspace_bytes(n, v, d), grad, stream)
+    _check(load().pdb_embed_grad(yp, ydt, ldy, kp, ix, n, gp, gdt, ldg, v, d, scale,
+                                 1 if accumulate else 0, _status(status, dev), wp, size,
+                                 _raw_stream(stream, dev)), "pdb_embed_grad")
     return grad
 
 
@@ -722,6 +730,7 @@ class TokenLogprobs:
         self.top_id, self.top_logp = top_id, top_logp
 
 
+@functools.lru_cache(maxsize=256)
 def pdb_token_logprobs_workspace_bytes(n: int, v: int, top: int = 0) -> int:
     out = ctypes.c_size_t(0)
     _check(load().pdb_token_logprobs_workspace_bytes(n, v, top, ctypes.byref(out)),
@@ -729,6 +738,7 @@ def pdb_token_logprobs_workspace_bytes(n: int, v: int, top: int = 0) -> int:
     return out.value
 
 
+@_on_own_device
 def pdb_token_logprobs(logits: torch.Tensor, tokens=None, top: int = 0, temp: float = 1.0, ws=None,
                        status=None, stream=None) -> TokenLogprobs:
     """Log probabilities of the given tokens (None: of none) under
@@ -736,21 +746,24 @@ def pdb_token_logprobs(logits: torch.Tensor, tokens=None, top: int = 0, temp: fl
     each row with their log probabilities, ties to the lowest index.  A row
     whose token is negative is skipped."""
     zp, zdt, ldz = _matrix(logits, "logits")
+    dev = logits.get_device()
     n, v = logits.shape
-    kp, ix = _tokens(tokens, n)
-    with _Call(logits.device, stream, tokens, ws, status) as c:
-        ws = c.workspace(ws, pdb_token_logprobs_workspace_bytes(n, v, top))
-        f = torch.float32
-        r = TokenLogprobs(None if tokens is None else c.empty(n, f), c.empty(n, f),
-                          c.empty((n, 2), f), c.empty((n, top), torch.int32) if top else None,
-                          c.empty((n, top), f) if top else None)
-        _check(load().pdb_token_logprobs(zp, zdt, ldz, n, v, kp, ix, temp, _ptr(r.logp),
-                                         _ptr(r.entropy), _ptr(r.stats), top, _ptr(r.top_id),
-                                         _ptr(r.top_logp), _status(status), _ptr(ws), ws.numel(),
-                                         c.stream), "pdb_token_logprobs")
-    return r
+    kp, ix = _tokens(tokens, n, dev)
+    wp, size, ws = _space(ws, pdb_token_logprobs_workspace_bytes(n, v, top), logits, stream)
+    f = torch.float32
+    logp = None if tokens is None else _empty(logits, n, f, stream)
+    entropy, stats = _empty(logits, n, f, stream), _empty(logits, (n, 2), f, stream)
+    top_id = _empty(logits, (n, top), torch.int32, stream) if top else None
+    top_logp = _empty(logits, (n, top), f, stream) if top else None
+    _check(load().pdb_token_logprobs(
+        zp, zdt, ldz, n, v, kp, ix, temp, logp.data_ptr() if logp is not None else None,
+        entropy.data_ptr(), stats.data_ptr(), top, top_id.data_ptr() if top else None,
+        top_logp.data_ptr() if top else None, _status(status, dev), wp, size,
+        _raw_stream(stream, dev)), "pdb_token_logprobs")
+    return TokenLogprobs(logp, entropy, stats, top_id, top_logp)
 
 
+@_on_own_device
 def pdb_token_logprobs_grad(logits: torch.Tensor, tokens, stats: torch.Tensor, d_logp=None,
                             entropy=None, d_entropy=None, temp: float = 1.0, out=None, status=None,
                             stream=None) -> torch.Tensor:
@@ -758,22 +771,23 @@ def pdb_token_logprobs_grad(logits: torch.Tensor, tokens, stats: torch.Tensor, d
     logits; stats and entropy from pdb_token_logprobs.  out: None, or where it
     goes (the logits themselves may be given)."""
     zp, zdt, ldz = _matrix(logits, "logits")
+    dev = logits.get_device()
     n, v = logits.shape
-    kp, ix = _tokens(tokens, n)
-    with _Call(logits.device, stream, tokens, stats, d_logp, entropy, d_entropy, out, status) as c:
-        if out is None:
-            out = c.empty((n, v), logits.dtype)
-        elif out.shape != logits.shape or out.dtype != logits.dtype:
-            raise ValueError("out must have the logits' shape and type")
-        op, _, ldd = _matrix(out, "out")
-        _check(load().pdb_token_logprobs_grad(
-            zp, zdt, ldz, n, v, kp, ix, temp, _vector(stats, "stats", 2 * n),
-            _vector(entropy, "entropy", n), _vector(d_logp, "d_logp", n),
-            _vector(d_entropy, "d_entropy", n), op, ldd, _status(status), c.stream),
-            "pdb_token_logprobs_grad")
+    kp, ix = _tokens(tokens, n, dev)
+    if out is None:
+        out = _empty(logits, (n, v), logits.dtype, stream)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and type")
+    op, _, ldd = _matrix(out, "out", dev)
+    _check(load().pdb_token_logprobs_grad(
+        zp, zdt, ldz, n, v, kp, ix, temp, _vector(stats, "stats", 2 * n, dev),
+        _vector(entropy, "entropy", n, dev), _vector(d_logp, "d_logp", n, dev),
+        _vector(d_entropy, "d_entropy", n, dev), op, ldd, _status(status, dev),
+        _raw_stream(stream, dev)), "pdb_token_logprobs_grad")
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def pdb_distill_workspace_bytes(n: int, v: int) -> int:
     out = ctypes.c_size_t(0)
     _check(load().pdb_distill_workspace_bytes(n, v, ctypes.byref(out)),
@@ -781,6 +795,7 @@ def pdb_distill_workspace_bytes(n: int, v: int) -> int:
     return out.value
 
 
+@_on_own_device
 def pdb_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temp: float = 1.0,
                 weight=None, grad: bool = True, out=None, ws=None, status=None, stream=None):
     """(loss [n], dlogits): each row's weighted divergence from the teacher's
@@ -789,6 +804,7 @@ def pdb_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, 
     (None without grad).  out: where the gradient goes (the logits themselves
     may be given)."""
     zp, zdt, ldz = _matrix(logits, "logits")
+    dev = logits.get_device()
     n, v = logits.shape
     if ids.dim() != 2 or ids.shape != teacher.shape or ids.shape[0] != n:
         raise ValueError("ids and teacher must be matrices of %d rows and equal shape" % n)
@@ -796,20 +812,20 @@ def pdb_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, 
     tdt = _DTYPES.get(teacher.dtype)
     if tdt is None:
         raise TypeError("teacher must be float32, float16 or bfloat16")
-    with _Call(logits.device, stream, ids, teacher, weight, out, ws, status) as c:
-        ws = c.workspace(ws, pdb_distill_workspace_bytes(n, v))
-        loss = c.empty(n, torch.float32)
-        op, ldd = None, 0
-        if grad:
-            if out is None:
-                out = c.empty((n, v), logits.dtype)
-            elif out.shape != logits.shape or out.dtype != logits.dtype:
-                raise ValueError("out must have the logits' shape and type")
-            op, _, ldd = _matrix(out, "out")
-        elif out is not None:
-            raise ValueError("out is for the gradient")
-        _check(load().pdb_distill(zp, zdt, ldz, n, v, _vector(ids, "ids", n * k, torch.int32),
-                                  _ptr(teacher), tdt, k, temp, _vector(weight, "weight", n),
-                                  _ptr(loss), op, ldd, _status(status), _ptr(ws), ws.numel(),
-                                  c.stream), "pdb_distill")
+    op, ldd = None, 0
+    if grad:
+        if out is None:
+            out = _empty(logits, (n, v), logits.dtype, stream)
+        elif out.shape != logits.shape or out.dtype != logits.dtype:
+            raise ValueError("out must have the logits' shape and type")
+        op, _, ldd = _matrix(out, "out", dev)
+    elif out is not None:
+        raise ValueError("out is for the gradient")
+    wp, size, ws = _space(ws, pdb_distill_workspace_bytes(n, v), logits, stream)
+    loss = _empty(logits, n, torch.float32, stream)
+    _check(load().pdb_distill(zp, zdt, ldz, n, v, _vector(ids, "ids", n * k, dev, torch.int32),
+                              _vector(teacher, "teacher", n * k, dev, teacher.dtype), tdt, k, temp,
+                              _vector(weight, "weight", n, dev), loss.data_ptr(), op, ldd,
+                              _status(status, dev), wp, size, _raw_stream(stream, dev)),
+           "pdb_distill")
     return loss, out
