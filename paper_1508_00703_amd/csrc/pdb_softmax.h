@@ -129,12 +129,14 @@ __device__ __forceinline__ Stat team_stat(Stat w, float c) {
     }
 }
 
-// a row's statistics from its parts', in part order, the same in every thread
+// A row's statistics from its parts', a part to a lane; the same in every thread.
+constexpr int64_t kMostParts = kWave;
 __device__ __forceinline__ Stat join_parts(const float *part_stat, int64_t i, int parts, float c) {
-    const float *q = part_stat + 3 * i * parts;
-    Stat t = {q[0], q[1], q[2]};
-    for (int k = 1; k < parts; ++k) t = join(t, Stat{q[3 * k], q[3 * k + 1], q[3 * k + 2]}, c);
-    return t;
+    const float *q = part_stat + 3 * (i * parts + lane_id());
+    Stat t = empty_stat();
+    if (lane_id() < parts) t = {q[0], q[1], q[2]};
+    rescale(t, wave_max_f32(t.m), c);
+    return {t.m, wave_sum64(t.s), wave_sum64(t.a)};
 }
 __device__ __forceinline__ void put_part(float *part_stat, int64_t w, const Stat &t) {
     part_stat[3 * w] = t.m;
@@ -314,7 +316,6 @@ struct Work {
 // How rows are cut into parts: up to kWantBlocks blocks when there are few rows
 // (four a compute unit), none with less than a tile.
 constexpr int64_t kWantBlocks = 1024;
-constexpr int64_t kMostParts = 64;
 struct Parts {
     int parts;
     int vecs;  // of a part

@@ -517,8 +517,11 @@ __global__ __launch_bounds__(kBlock) void k_logprobs_join(LogprobArgs p) {
         if (threadIdx.x == 0) s_top.n = 0;
         __syncthreads();
         if (count <= TopLds<kW>::kRanked) {
+            // no worse than any part's K-th best
+            const int last = (lane_id() + 1) * p.top - 1;
+            const uint32_t least = max(wave_max_u32(lane_id() < p.parts ? from[2 * last] : 0), 1u);
             for (int k = threadIdx.x; k < count; k += kBlock)
-                if (from[2 * k] > 0) push(s_top, from[2 * k], from[2 * k + 1]);
+                if (from[2 * k] >= least) push(s_top, from[2 * k], from[2 * k + 1]);
         } else {
             constexpr int kN = kJoin / kBlock;
             uint32_t key[kN], at[kN];
