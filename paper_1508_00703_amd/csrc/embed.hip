@@ -94,8 +94,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 // to 16 x 1024 tokens, each wave a stretch of it, and ranks them by ballots (a hot
 // token costs nothing extra).  A pass is two launches, the tiles' digit counts and
 // the move, each block summing the counts of all tiles by itself, which takes no
-// scan launches; past kSortTiles that reading grows too long and the library's own
-// sort runs.
+// scan launches; past kSortTiles that reading grows too long and the general sort
+// of pdb_internal.h runs.
 
 constexpr int kSortBlock = 1024;
 constexpr int kSortItems = 16;
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_move(
     }
 }
 
-// tokens to sort keys, for the library's sort
+// tokens to sort keys, for the general sort
 __global__ __launch_bounds__(kBlock) void k_token_keys(const void *__restrict__ tokens, int index,
                                                        int64_t n, int64_t v,
                                                        uint32_t *__restrict__ keys,
