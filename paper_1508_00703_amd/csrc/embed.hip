@@ -93,34 +93,45 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 // launch.  More go through a radix sort: a block of 1024 threads takes a tile of up
 // to 16 x 1024 tokens, each wave a stretch of it, and ranks them by ballots (a hot
 // token costs nothing extra).  A pass is two launches, the tiles' digit counts and
-// the move, each block summing the counts of all tiles by itself, which takes no
-// scan launches; past kSortTiles that reading grows too long and the general sort
-// of pdb_internal.h runs.
+// the move, each block summing the counts of all tiles by itself; where that reading
+// grows too long a scan of the counts stands between them, and past kSortTiles the
+// general sort of pdb_internal.h runs.  Digits have up to 10 bits, so that 2^20 rows
+// take two passes: 101 us for 4M tokens, against 117 us in three passes of 7 bits (a
+// wider digit moves 33 us instead of 28, in shorter runs), with the sums 256 us
+// against 270; 1M tokens of 100,000 rows and 64 bf16 columns 95 us against 107.
 
 constexpr int kSortBlock = 1024;
 constexpr int kSortItems = 16;
 constexpr int kSortTile = kSortBlock * kSortItems;
 constexpr int kSortTiles = 512;
+constexpr int kDigitBits = 10;  // of the widest digit
+constexpr int kDigits = 1 << kDigitBits;
 
 struct SortLds {
-    uint32_t key[kSortTile], val[kSortTile];
-    uint32_t cnt[kSortBlock / kWave][256];  // per wave and digit: a count, then where its run starts
-    uint32_t start[256];                    // per digit: where it starts in the tile
-    uint32_t out[256], all[256];            // per digit: where it goes; all tiles' count
-    uint32_t wave[4];
+    union {
+        struct {
+            uint32_t key[kSortTile], val[kSortTile];
+        };
+        // per wave and digit: a count, then where its run starts
+        uint32_t cnt[kSortBlock / kWave][kDigits];
+    };
+    uint32_t start[kDigits];                // per digit: where it starts in the tile
+    uint32_t out[kDigits], all[kDigits];    // per digit: where it goes; all tiles' count
+    uint32_t wave[kSortBlock / kWave];
 };
 
 __device__ __forceinline__ uint32_t digit_of(uint32_t key, int shift, int nb) {
     return (key >> shift) & ((1u << nb) - 1u);
 }
 // The lanes that hold the same digit: of each bit's ballot, or its complement,
-// by the lane's own bit spread over a word.  All 8 bits of a digit are looked at
+// by the lane's own bit spread over a word.  All B bits of a digit are looked at
 // (those above nb are 0): unrolled, they take half the instructions of a loop.
+template <int B>
 __device__ __forceinline__ unsigned long long digit_peers(uint32_t dg, bool valid) {
     const unsigned long long there = __ballot(valid);
     uint32_t lo = (uint32_t)there, hi = (uint32_t)(there >> 32);
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
+    for (int b = 0; b < B; ++b) {
         const uint32_t own = (uint32_t)__builtin_amdgcn_sbfe((int)dg, b, 1);
         const unsigned long long set = __ballot(own != 0);
         lo &= ~((uint32_t)set ^ own);
@@ -129,15 +140,14 @@ __device__ __forceinline__ unsigned long long digit_peers(uint32_t dg, bool vali
     return (unsigned long long)hi << 32 | lo;
 }
 
-// exclusive prefix sum over the first 256 threads of the block
-__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t *s_wave) {
+// exclusive prefix sum over the block's threads
+__device__ __forceinline__ uint32_t scan_block(uint32_t v, uint32_t *s_wave) {
     const uint32_t incl = wave_incl_scan_u32(v);
     const int w = wave_in_block();
-    if (w < 4 && lane_id() == kWave - 1) s_wave[w] = incl;
+    if (lane_id() == kWave - 1) s_wave[w] = incl;
     __syncthreads();
-    uint32_t before = 0;
-    for (int k = 0; k < min(w, 4); ++k) before += s_wave[k];
-    return before + incl - v;
+    const uint32_t of_wave = lane_id() < w ? s_wave[lane_id()] : 0;  // the waves before
+    return wave_sum_u32(of_wave) + incl - v;
 }
 
 // Item j of a thread is entry (wave * items + j) * 64 + lane of the tile.
@@ -145,19 +155,20 @@ __device__ __forceinline__ int tile_entry(int items, int j) {
     return (wave_in_block() * items + j) * kWave + lane_id();
 }
 
-// The place of each item in the tile by its digit, items of one digit in order.
+// The place of each item in the tile by its digit (of up to B bits), items of one
+// digit in order.
+template <int B>
 __device__ __forceinline__ void rank_tile(SortLds &S, const uint32_t *k, int items, int count,
                                           int shift, int nb, uint32_t *pos) {
     const int t = threadIdx.x, w = wave_in_block(), radix = 1 << nb;
-    for (int i = t; i < (int)sizeof(S.cnt) / 4; i += kSortBlock)
-        reinterpret_cast<uint32_t *>(S.cnt)[i] = 0;
+    for (int i = lane_id(); i < radix; i += kWave) S.cnt[w][i] = 0;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {
         if (j >= items) continue;
         const bool valid = tile_entry(items, j) < count;
         const uint32_t dg = digit_of(k[j], shift, nb);
-        const unsigned long long peers = digit_peers(dg, valid);
+        const unsigned long long peers = digit_peers<B>(dg, valid);
         const unsigned r = lanes_below(peers);
         // of the wave's items before this one (a wave's LDS accesses run in order)
         const uint32_t before =
@@ -179,8 +190,8 @@ __device__ __forceinline__ void rank_tile(SortLds &S, const uint32_t *k, int ite
             sum += c;
         }
     }
-    const uint32_t start = scan256(sum, S.wave);
-    if (t < 256) S.start[t] = start;
+    const uint32_t start = scan_block(sum, S.wave);
+    if (t < radix) S.start[t] = start;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {
@@ -260,11 +271,13 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_count(
     uint32_t *__restrict__ keys, int64_t n, int items, int shift, int nb,
     uint32_t *__restrict__ hist) {
     constexpr int kCopies = 4;  // of the counts, for a quarter of the waves each
-    __shared__ uint32_t s_cnt[kCopies][256];
+    __shared__ uint32_t s_cnt[kCopies][kDigits];
     const int t = threadIdx.x;
     uint32_t *mine = s_cnt[wave_in_block() % kCopies];
-    (&s_cnt[0][0])[t] = 0;
-    static_assert(kCopies * 256 == kSortBlock, "one count a thread");
+    if (t < (1 << nb))
+#pragma unroll
+        for (int q = 0; q < kCopies; ++q) s_cnt[q][t] = 0;
+    static_assert(kDigits <= kSortBlock, "a digit a thread");
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * items * kSortBlock;
     uint32_t k[kSortItems];
@@ -300,11 +313,42 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_count(
     }
 }
 
-// One pass: vals_in NULL means value = position.
+// Of many tiles or wide digits: each digit's count in the tiles before, in place of
+// its counts, and behind the last tile its count in all.  A lane has a digit, a wave
+// every 16th part of the tiles.
+constexpr int kScanTiles = kSortTiles / (kSortBlock / kWave);
+__global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__restrict__ hist,
+                                                                int tiles, int nb) {
+    __shared__ uint32_t s_sum[kSortBlock / kWave][kWave];
+    const int w = wave_in_block(), lane = lane_id(), d = (int)blockIdx.x * kWave + lane;
+    const int per = (tiles + kSortBlock / kWave - 1) / (kSortBlock / kWave);
+    const int from = w * per, to = min(tiles, from + per);
+    uint32_t c[kScanTiles], sum = 0;
+#pragma unroll
+    for (int q = 0; q < kScanTiles; ++q)
+        c[q] = from + q < to ? hist[((int64_t)(from + q) << nb) + d] : 0;
+#pragma unroll
+    for (int q = 0; q < kScanTiles; ++q) sum += c[q];
+    s_sum[w][lane] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+#pragma unroll
+    for (int q = 0; q < kSortBlock / kWave; ++q) before += q < w ? s_sum[q][lane] : 0;
+#pragma unroll
+    for (int q = 0; q < kScanTiles; ++q) {
+        if (from + q < to) hist[((int64_t)(from + q) << nb) + d] = before;
+        before += c[q];
+    }
+    if (w == kSortBlock / kWave - 1) hist[((int64_t)tiles << nb) + d] = before;
+}
+
+// One pass, on digits of up to B bits: vals_in NULL means value = position.  scanned:
+// hist is as k_token_sort_scan leaves it.
+template <int B>
 __global__ __launch_bounds__(kSortBlock) void k_token_sort_move(
     const uint32_t *__restrict__ keys_in, const uint32_t *__restrict__ vals_in, int64_t n, int items,
-    int shift, int nb, const uint32_t *__restrict__ hist, int tiles, uint32_t *__restrict__ keys,
-    uint32_t *__restrict__ vals) {
+    int shift, int nb, const uint32_t *__restrict__ hist, int tiles, bool scanned,
+    uint32_t *__restrict__ keys, uint32_t *__restrict__ vals) {
     __shared__ SortLds S;
     const int t = threadIdx.x, radix = 1 << nb;
     const int64_t base = (int64_t)blockIdx.x * items * kSortBlock;
@@ -319,22 +363,32 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_move(
     }
     // where each digit of this tile goes: every smaller digit, and this one in
     // the tiles before
-    if (t < 256) S.all[t] = S.out[t] = 0;
-    __syncthreads();
-    uint32_t all = 0, before = 0;
+    uint32_t mine = 0, all = 0;
+    if (scanned) {
+        if (t < radix) {
+            mine = hist[((int64_t)blockIdx.x << nb) + t];
+            all = hist[((int64_t)tiles << nb) + t];
+        }
+    } else {
+        if (t < radix) S.all[t] = S.out[t] = 0;
+        __syncthreads();
 #pragma unroll 8
-    for (int q = t >> nb; q < tiles; q += kSortBlock >> nb) {
-        const uint32_t c = hist[((int64_t)q << nb) + (t & (radix - 1))];
-        all += c;
-        before += q < (int)blockIdx.x ? c : 0;
+        for (int q = t >> nb; q < tiles; q += kSortBlock >> nb) {
+            const uint32_t c = hist[((int64_t)q << nb) + (t & (radix - 1))];
+            all += c;
+            mine += q < (int)blockIdx.x ? c : 0;
+        }
+        atomicAdd(&S.all[t & (radix - 1)], all);
+        atomicAdd(&S.out[t & (radix - 1)], mine);
+        __syncthreads();
+        mine = t < radix ? S.out[t] : 0;
+        all = t < radix ? S.all[t] : 0;
     }
-    atomicAdd(&S.all[t & (radix - 1)], all);
-    atomicAdd(&S.out[t & (radix - 1)], before);
+    const uint32_t smaller = scan_block(all, S.wave);
+    if (t < radix) S.out[t] = mine + smaller;
     __syncthreads();
-    const uint32_t smaller = scan256(t < radix ? S.all[t] : 0, S.wave);
-    if (t < radix) S.out[t] += smaller;
-    __syncthreads();
-    rank_tile(S, k, items, count, shift, nb, pos);
+    rank_tile<B>(S, k, items, count, shift, nb, pos);
+    __syncthreads();  // the counts' place is the tile's now
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {
         if (j >= items) continue;
@@ -812,13 +866,16 @@ GradWs grad_ws_layout(void *base, int64_t n, int64_t d) {
         w.keys = reinterpret_cast<uint32_t *>(take(4 * n));
         w.kB = reinterpret_cast<uint32_t *>(take(4 * n));
         w.vB = reinterpret_cast<uint32_t *>(take(4 * n));
-        w.hist = reinterpret_cast<uint32_t *>(take(4 * 256 * std::max<int64_t>(st, kSortTiles)));
+        w.hist = reinterpret_cast<uint32_t *>(take(std::max<int64_t>(4 * 256 * st, 4 * kDigits * (kSortTiles + 1))));
         w.scan_tmp = reinterpret_cast<uint32_t *>(take(4 * (int64_t)scan_tmp_elems(256 * st)));
     }
     w.part = reinterpret_cast<float *>(take(spans * 2 * d * 4));
     w.total = off;
     return w;
 }
+
+// Counts that every block of the move sums by itself; more go through a scan.
+constexpr int64_t kDirectCounts = 1 << 15;
 
 // The tokens in order (padding as v, last) and their positions.
 int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64_t v,
@@ -844,7 +901,7 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
     // about 128 tiles: half of the compute units, and counts that are soon summed
     const int items = (int)std::min<int64_t>(kSortItems, cdiv(n, 128 * kSortBlock));
     const int tiles = (int)cdiv(n, (int64_t)items * kSortBlock);
-    const int passes = (bits + 7) / 8, step = (bits + passes - 1) / passes;
+    const int passes = (bits + kDigitBits - 1) / kDigitBits, step = (bits + passes - 1) / passes;
     const uint32_t *ck = w.keys, *cv = nullptr;
     for (int shift = 0; shift < bits; shift += step) {
         const int nb = std::min(step, bits - shift);
@@ -855,9 +912,18 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
             k_token_sort_count<false><<<tiles, kSortBlock, 0, s>>>(
                 nullptr, 0, v, nullptr, const_cast<uint32_t *>(ck), n, items, shift, nb, w.hist);
         PDB_LAUNCHED();
+        const bool scan = nb >= 6 && (int64_t)tiles << nb > kDirectCounts;
+        if (scan) {
+            k_token_sort_scan<<<1 << (nb - 6), kSortBlock, 0, s>>>(w.hist, tiles, nb);
+            PDB_LAUNCHED();
+        }
         uint32_t *tk = ck == w.kA ? w.kB : w.kA, *tv = ck == w.kA ? w.vB : w.vA;
-        k_token_sort_move<<<tiles, kSortBlock, 0, s>>>(ck, cv, n, items, shift, nb, w.hist, tiles,
-                                                       tk, tv);
+        if (nb <= 8)
+            k_token_sort_move<8><<<tiles, kSortBlock, 0, s>>>(ck, cv, n, items, shift, nb, w.hist,
+                                                              tiles, scan, tk, tv);
+        else
+            k_token_sort_move<kDigitBits><<<tiles, kSortBlock, 0, s>>>(
+                ck, cv, n, items, shift, nb, w.hist, tiles, scan, tk, tv);
         PDB_LAUNCHED();
         ck = tk;
         cv = tv;
