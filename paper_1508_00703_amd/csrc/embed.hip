@@ -96,14 +96,17 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 // the move, each block summing the counts of all tiles by itself; where that reading
 // grows too long a scan of the counts stands between them, and past kSortTiles the
 // general sort of pdb_internal.h runs.  Digits have up to 10 bits, so that 2^20 rows
-// take two passes: 101 us for 4M tokens, against 117 us in three passes of 7 bits (a
-// wider digit moves 33 us instead of 28, in shorter runs), with the sums 256 us
-// against 270; 1M tokens of 100,000 rows and 64 bf16 columns 95 us against 107.
+// take two passes, of 33 us where 7 bits took 28, in shorter runs.  4M tokens of rank
+// 32, sort and sums: 270 us in three passes of 7 bits, 256 in two of 10, 252 where the
+// first pass reads the tokens twice instead of leaving their keys, 245 with the blocks
+// dealt to the dies as tile_of_block says.  Tiles of 8,192 tokens, two to a compute
+// unit, are slower: 311.
 
 constexpr int kSortBlock = 1024;
 constexpr int kSortItems = 16;
 constexpr int kSortTile = kSortBlock * kSortItems;
 constexpr int kSortTiles = 512;
+constexpr int64_t kSortMost = (int64_t)kSortTiles * kSortTile;
 constexpr int kDigitBits = 10;  // of the widest digit
 constexpr int kDigits = 1 << kDigitBits;
 
@@ -263,39 +266,46 @@ __global__ __launch_bounds__(kSortBlock) void k_token_rank(const void *__restric
     }
 }
 
-// Digit counts of each tile, [tile][digit].  FIRST reads the tokens and leaves
-// their keys.
+// The keys that a pass sorts: of the tokens (FIRST), or as the pass before left them.
+struct SortIn {
+    const void *tokens;
+    int index;
+    int64_t v;
+    int32_t *status;
+    const uint32_t *keys, *vals;
+    int64_t n;
+    int items, shift, nb, tiles;
+};
 template <bool FIRST>
-__global__ __launch_bounds__(kSortBlock) void k_token_sort_count(
-    const void *__restrict__ tokens, int index, int64_t v, int32_t *status,
-    uint32_t *__restrict__ keys, int64_t n, int items, int shift, int nb,
-    uint32_t *__restrict__ hist) {
+__device__ __forceinline__ uint32_t sort_key(const SortIn &in, int64_t i, int32_t *status) {
+    return FIRST ? token_key(in.tokens, in.index, i, in.v, status) : in.keys[i];
+}
+
+// Digit counts of each tile, [tile][digit].
+template <bool FIRST>
+__global__ __launch_bounds__(kSortBlock) void k_token_sort_count(SortIn in,
+                                                                 uint32_t *__restrict__ hist) {
     constexpr int kCopies = 4;  // of the counts, for a quarter of the waves each
     __shared__ uint32_t s_cnt[kCopies][kDigits];
     const int t = threadIdx.x;
     uint32_t *mine = s_cnt[wave_in_block() % kCopies];
-    if (t < (1 << nb))
+    if (t < (1 << in.nb))
 #pragma unroll
         for (int q = 0; q < kCopies; ++q) s_cnt[q][t] = 0;
     static_assert(kDigits <= kSortBlock, "a digit a thread");
     __syncthreads();
-    const int64_t base = (int64_t)blockIdx.x * items * kSortBlock;
+    const int64_t base = (int64_t)blockIdx.x * in.items * kSortBlock;
     uint32_t k[kSortItems];
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {  // all loads before the first is used
         const int64_t i = base + j * kSortBlock + t;
-        k[j] = 0;
-        if (j < items && i < n)
-            k[j] = FIRST ? token_key(tokens, index, i, v, status) : keys[i];
+        k[j] = j < in.items && i < in.n ? sort_key<FIRST>(in, i, in.status) : 0;
     }
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {
-        if (j >= items) continue;
-        const int64_t i = base + j * kSortBlock + t;
-        const bool valid = i < n;
-        const uint32_t key = k[j];
-        if (FIRST && valid) keys[i] = key;
-        const uint32_t dg = digit_of(key, shift, nb);
+        if (j >= in.items) continue;
+        const bool valid = base + j * kSortBlock + t < in.n;
+        const uint32_t dg = digit_of(k[j], in.shift, in.nb);
         // a digit that many lanes hold is counted once for all of them: adds to one
         // LDS address go one after another
         const uint32_t d0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)dg);
@@ -305,11 +315,11 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_count(
         if (valid && !(hot && dg == d0)) atomicAdd(&mine[dg], 1u);
     }
     __syncthreads();
-    if (t < (1 << nb)) {
+    if (t < (1 << in.nb)) {
         uint32_t all = 0;
 #pragma unroll
         for (int q = 0; q < kCopies; ++q) all += s_cnt[q][t];
-        hist[((int64_t)blockIdx.x << nb) + t] = all;
+        hist[((int64_t)blockIdx.x << in.nb) + t] = all;
     }
 }
 
@@ -342,31 +352,38 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__rest
     if (w == kSortBlock / kWave - 1) hist[((int64_t)tiles << nb) + d] = before;
 }
 
-// One pass, on digits of up to B bits: vals_in NULL means value = position.  scanned:
+// Block b's tile: the blocks of one die (b mod 8) have neighbouring tiles, whose
+// stretches of a digit lie next to each other and meet in that die's cache.
+__device__ __forceinline__ int tile_of_block(int b, int tiles) {
+    const int die = b & 7;
+    return die * (tiles >> 3) + min(die, tiles & 7) + (b >> 3);
+}
+
+// One pass, on digits of up to B bits; the first one's values are positions.  scanned:
 // hist is as k_token_sort_scan leaves it.
-template <int B>
+template <int B, bool FIRST>
 __global__ __launch_bounds__(kSortBlock) void k_token_sort_move(
-    const uint32_t *__restrict__ keys_in, const uint32_t *__restrict__ vals_in, int64_t n, int items,
-    int shift, int nb, const uint32_t *__restrict__ hist, int tiles, bool scanned,
-    uint32_t *__restrict__ keys, uint32_t *__restrict__ vals) {
+    SortIn in, const uint32_t *__restrict__ hist, bool scanned, uint32_t *__restrict__ keys,
+    uint32_t *__restrict__ vals) {
     __shared__ SortLds S;
-    const int t = threadIdx.x, radix = 1 << nb;
-    const int64_t base = (int64_t)blockIdx.x * items * kSortBlock;
-    const int count = (int)min((int64_t)items * kSortBlock, n - base);
+    const int items = in.items, shift = in.shift, nb = in.nb, tiles = in.tiles;
+    const int t = threadIdx.x, radix = 1 << nb, tile = tile_of_block((int)blockIdx.x, tiles);
+    const int64_t base = (int64_t)tile * items * kSortBlock;
+    const int count = (int)min((int64_t)items * kSortBlock, in.n - base);
     uint32_t k[kSortItems], p[kSortItems], pos[kSortItems];
 #pragma unroll
     for (int j = 0; j < kSortItems; ++j) {
         if (j >= items) continue;
         const int e = tile_entry(items, j);
-        k[j] = e < count ? keys_in[base + e] : 0;
-        p[j] = e < count ? (vals_in ? vals_in[base + e] : (uint32_t)(base + e)) : 0;
+        k[j] = e < count ? sort_key<FIRST>(in, base + e, nullptr) : 0;
+        p[j] = FIRST ? (uint32_t)(base + e) : e < count ? in.vals[base + e] : 0;
     }
     // where each digit of this tile goes: every smaller digit, and this one in
     // the tiles before
     uint32_t mine = 0, all = 0;
     if (scanned) {
         if (t < radix) {
-            mine = hist[((int64_t)blockIdx.x << nb) + t];
+            mine = hist[((int64_t)tile << nb) + t];
             all = hist[((int64_t)tiles << nb) + t];
         }
     } else {
@@ -376,7 +393,7 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_move(
         for (int q = t >> nb; q < tiles; q += kSortBlock >> nb) {
             const uint32_t c = hist[((int64_t)q << nb) + (t & (radix - 1))];
             all += c;
-            mine += q < (int)blockIdx.x ? c : 0;
+            mine += q < tile ? c : 0;
         }
         atomicAdd(&S.all[t & (radix - 1)], all);
         atomicAdd(&S.out[t & (radix - 1)], mine);
@@ -863,7 +880,7 @@ GradWs grad_ws_layout(void *base, int64_t n, int64_t d) {
     w.kA = reinterpret_cast<uint32_t *>(take(4 * n));
     w.vA = reinterpret_cast<uint32_t *>(take(4 * n));
     if (n > kRankTokens) {
-        w.keys = reinterpret_cast<uint32_t *>(take(4 * n));
+        if (n > kSortMost) w.keys = reinterpret_cast<uint32_t *>(take(4 * n));
         w.kB = reinterpret_cast<uint32_t *>(take(4 * n));
         w.vB = reinterpret_cast<uint32_t *>(take(4 * n));
         w.hist = reinterpret_cast<uint32_t *>(take(std::max<int64_t>(4 * 256 * st, 4 * kDigits * (kSortTiles + 1))));
@@ -890,7 +907,7 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
         PDB_LAUNCHED();
         return PDB_OK;
     }
-    if (n > (int64_t)kSortTiles * kSortTile) {
+    if (n > kSortMost) {
         k_token_keys<<<grid_for(n, kBlock, 4096), kBlock, 0, s>>>(tokens, index, n, v, w.keys,
                                                                   status);
         PDB_LAUNCHED();
@@ -902,33 +919,34 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
     const int items = (int)std::min<int64_t>(kSortItems, cdiv(n, 128 * kSortBlock));
     const int tiles = (int)cdiv(n, (int64_t)items * kSortBlock);
     const int passes = (bits + kDigitBits - 1) / kDigitBits, step = (bits + passes - 1) / passes;
-    const uint32_t *ck = w.keys, *cv = nullptr;
-    for (int shift = 0; shift < bits; shift += step) {
-        const int nb = std::min(step, bits - shift);
-        if (shift == 0)
-            k_token_sort_count<true><<<tiles, kSortBlock, 0, s>>>(tokens, index, v, status, w.keys,
-                                                                  n, items, shift, nb, w.hist);
+    SortIn in = {tokens, index, v, status, nullptr, nullptr, n, items, 0, 0, tiles};
+    for (; in.shift < bits; in.shift += step) {
+        const int nb = in.nb = std::min(step, bits - in.shift);
+        const bool first = in.shift == 0;
+        if (first)
+            k_token_sort_count<true><<<tiles, kSortBlock, 0, s>>>(in, w.hist);
         else
-            k_token_sort_count<false><<<tiles, kSortBlock, 0, s>>>(
-                nullptr, 0, v, nullptr, const_cast<uint32_t *>(ck), n, items, shift, nb, w.hist);
+            k_token_sort_count<false><<<tiles, kSortBlock, 0, s>>>(in, w.hist);
         PDB_LAUNCHED();
         const bool scan = nb >= 6 && (int64_t)tiles << nb > kDirectCounts;
         if (scan) {
             k_token_sort_scan<<<1 << (nb - 6), kSortBlock, 0, s>>>(w.hist, tiles, nb);
             PDB_LAUNCHED();
         }
-        uint32_t *tk = ck == w.kA ? w.kB : w.kA, *tv = ck == w.kA ? w.vB : w.vA;
-        if (nb <= 8)
-            k_token_sort_move<8><<<tiles, kSortBlock, 0, s>>>(ck, cv, n, items, shift, nb, w.hist,
-                                                              tiles, scan, tk, tv);
+        uint32_t *tk = in.keys == w.kA ? w.kB : w.kA, *tv = in.keys == w.kA ? w.vB : w.vA;
+        if (nb <= 8 && first)
+            k_token_sort_move<8, true><<<tiles, kSortBlock, 0, s>>>(in, w.hist, scan, tk, tv);
+        else if (nb <= 8)
+            k_token_sort_move<8, false><<<tiles, kSortBlock, 0, s>>>(in, w.hist, scan, tk, tv);
+        else if (first)
+            k_token_sort_move<kDigitBits, true><<<tiles, kSortBlock, 0, s>>>(in, w.hist, scan, tk,
+                                                                             tv);
         else
-            k_token_sort_move<kDigitBits><<<tiles, kSortBlock, 0, s>>>(
-                ck, cv, n, items, shift, nb, w.hist, tiles, scan, tk, tv);
+            k_token_sort_move<kDigitBits, false><<<tiles, kSortBlock, 0, s>>>(in, w.hist, scan, tk,
+                                                                              tv);
         PDB_LAUNCHED();
-        ck = tk;
-        cv = tv;
-        *keys = tk;
-        *vals = tv;
+        in.keys = *keys = tk;
+        in.vals = *vals = tv;
     }
     return PDB_OK;
 }
