@@ -337,12 +337,13 @@ inline unsigned blocks_for(int64_t work, int per_block = 1) {
 }
 // A wave to a row, instead of a block.  Rows of few vectors leave a block's threads
 // idle (16,384 rows of 4,000 bf16: 30 us against 49, with the gradient 45 against 51;
-// of 8,000 the block is even or ahead).  With a selection, whose cost is the wave's,
-// also longer rows where every compute unit still has sixteen (8,192 of 32,768 with 64
-// alternatives: 161 us against 184; without any 108 against 96).
+// of 8,000 the block is even or ahead).  With a selection, which costs each wave and
+// joins a block's, also longer rows where every compute unit still has eight (3,000 of
+// 40,000 with 5 alternatives: 58 us against 66, 8,192 of 32,768 with 64: 156 against
+// 165; 1,600 of 65,536 with 1: 61 against 55).
 inline bool wave_rows(const Parts &cut, int64_t n, int64_t v, int64_t vec, bool selection) {
     if (cut.parts > 1) return false;
-    return v <= vec * (selection ? 1024 : 512) || (selection && n >= 4096);
+    return v <= vec * (selection ? 1024 : 512) || (selection && n >= 2048);
 }
 
 }  // namespace pdbk

@@ -18,12 +18,15 @@ namespace {
 // 1 is NaN, 0 nothing.  The row's K best lie in the K best of its vectors, ordered
 // by (largest key, index): an element of any other has K better ones.  So while a
 // row streams by, only its vectors' maxima are looked at: those better than a bound
-// are kept in LDS.  The bound is the K-th best of K or more vectors met so far.
-// The first tile sets it, from the K-th best of a wave's vectors; when the kept ones
-// would overflow, it is raised to the K-th best of those kept and the tile's, which
-// leaves K, whatever the data.  The K vectors that remain are read again, and their
-// elements put in order.  The K-th best of a set spread over the team is found by a
-// binary search over the bits of its key, counting with ballots.
+// are kept in LDS, by each wave in a place of its own, so that the waves of a team
+// wait for each other at a row's ends only (with a barrier every tile, 1,000 rows of
+// 100,003 in 32 bits took 90 us with 64 alternatives, now 83).  The bound is the K-th
+// best of K or more vectors met so far.  The first tile sets it, from the K-th best of
+// a wave's vectors, or from the (K / W)-th best of each of W waves'; when a wave's
+// kept ones would overflow, its bound is raised to the K-th best of those kept and the
+// tile's, which leaves K, whatever the data.  Of the vectors kept in the end the K best
+// are read again, and their elements and the row's tail put in order.  The K-th best of
+// a set is found by a binary search over the bits of its key, counting with ballots.
 
 template <int DT>
 struct Key {
@@ -120,20 +123,21 @@ __device__ __forceinline__ uint64_t candidate(uint32_t key, uint32_t at) {
 __device__ __forceinline__ uint32_t key_of(uint64_t c) { return (uint32_t)(c >> 32); }
 __device__ __forceinline__ uint32_t index_of(uint64_t c) { return ~(uint32_t)c; }
 
-// Room of a team's selection: vectors kept while a row streams by, elements of the K
-// vectors in the end (8 K), candidates that are ranked against each other.
+// Room of a team's selection: vectors that each wave keeps while a row streams by,
+// elements of the K vectors in the end (8 K, and a tail's 7), candidates that are
+// ranked against each other.
 template <int W>
 struct TopLds {
     static constexpr int kTop = W == 1 ? PDB_MAX_TOP / 2 : PDB_MAX_TOP;  // largest K
-    static constexpr int kKeep = W == 1 ? 256 : 512;
+    static constexpr int kKeep = 256;                                    // a wave's
     static constexpr int kCand = kTop * 8;
     static constexpr int kRanked = 512;
-    static_assert(kCand >= kKeep && kCand >= kRanked, "c holds each");
+    static_assert(kCand >= W * kKeep && kCand >= kRanked && kKeep >= kTop, "c holds each");
     alignas(16) uint64_t c[kCand + 8];
     uint32_t rank[kRanked];
     int n;
-    int add[3];  // candidates of a tile, in turn
-    uint32_t wave[W];
+    int held[W];                // vectors that each wave has kept
+    uint32_t first[W], last[W];  // each wave's bound, of its first tile and in the end
 };
 
 template <int W>
@@ -147,10 +151,11 @@ inline int bits_for(int64_t count) {
     return b;
 }
 
-// The k best of the first n <= M candidates in L and of the given ones stay in L,
-// L.n of them; returns the bound.  Every thread of the team calls.
+// The k best of the first n <= M candidates in c and of the given ones stay in c,
+// `count` of them; returns the bound.  Every thread of the team calls.
 template <int DT, int W, int M, int N>
-__device__ __forceinline__ Bound keep_best(TopLds<W> &L, int n, const uint32_t (&more)[N],
+__device__ __forceinline__ Bound keep_best(uint64_t *c, int &count, int n,
+                                           const uint32_t (&more)[N],
                                            const uint32_t (&more_at)[N], int k, int at_bits) {
     constexpr int kT = Team<W>::kThreads, kN = M / kT;
     static_assert(M % kT == 0, "whole rounds");
@@ -160,20 +165,21 @@ __device__ __forceinline__ Bound keep_best(TopLds<W> &L, int n, const uint32_t (
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
         const int q = i * kT + t;
-        key[i] = q < n ? key_of(L.c[q]) : 0;
-        at[i] = q < n ? index_of(L.c[q]) : 0;
+        key[i] = q < n ? key_of(c[q]) : 0;
+        at[i] = q < n ? index_of(c[q]) : 0;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         key[kN + i] = more[i];
         at[kN + i] = more_at[i];
     }
-    if (t == 0) L.n = 0;
+    if (t == 0) count = 0;
     const Bound b = kth_best<DT, W, kN + N>(key, at, k, at_bits);
     Team<W>::sync();
 #pragma unroll
     for (int i = 0; i < kN + N; ++i)
-        if (key[i] > 0 && passes(b, key[i], at[i])) push(L, key[i], at[i]);
+        if (key[i] > 0 && passes(b, key[i], at[i]))
+            c[atomicAdd(&count, 1)] = candidate(key[i], at[i]);
     Team<W>::sync();
     return b;
 }
@@ -184,23 +190,19 @@ struct Selection {
     using Lds = TopLds<W>;
     static constexpr int kV = Elem<DT>::kVec;
     static constexpr int kT = Team<W>::kThreads;
+    // the wave's
     uint32_t bound;  // its key
     float least;     // its logit: what is not larger is not kept; NaN: everything is
-    int n;           // vectors in L
+    int n;           // vectors kept
 
-    // every thread; L is free.  tail: this thread's element of the row's tail, of rem,
-    // which stands as vector `full`
-    __device__ __forceinline__ void start(Lds &L, float tail, int full, int rem) {
+    static __device__ __forceinline__ uint64_t *kept(Lds &L) {
+        return L.c + Team<W>::wave() * Lds::kKeep;
+    }
+
+    __device__ __forceinline__ void start() {
         bound = 0;
         least = kNan;
-        n = rem > 0 ? 1 : 0;
-        const int t = Team<W>::thread();
-        if (W > 1 && t < 3) L.add[t] = 0;
-        if (rem > 0 && Team<W>::wave() == 0) {
-            const uint32_t best = wave_max_u32(t < rem ? rank_key<DT>(tail) : 0);
-            if (t == 0) L.c[0] = candidate(best, (uint32_t)full);
-        }
-        Team<W>::sync();
+        n = 0;
     }
 
     // The largest logit under a key: where the bound comes from this very tile,
@@ -243,18 +245,31 @@ struct Selection {
         uint32_t key[kTileVecs];
 #pragma unroll
         for (int u = 0; u < kTileVecs; ++u) key[u] = j + u * kT < end ? rank_key<DT>(lm[u]) : 0;
-        if (k <= kWave / 2) {
+        const int share = (k + W - 1) / W;
+        if (share <= kWave / 2) {
             const uint32_t own[1] = {max(max(key[0], key[1]), max(key[2], key[3]))};
             static_assert(kTileVecs == 4, "four vectors");
-            bound = wave_bound(own, k);
+            bound = wave_bound(own, share);
         } else {
-            bound = wave_bound(key, k);
+            bound = wave_bound(key, share);
         }
-        if constexpr (W > 1) {  // the best of the waves'
-            if (lane_id() == 0) L.wave[wave_in_block()] = bound;
+        if constexpr (W > 1) {
+            // every wave has `share` no worse than its own: the waves of which k / share
+            // have no lesser bound than one have k no worse than that one
+            if (lane_id() == 0) L.first[wave_in_block()] = bound;
             __syncthreads();
+            const int waves = (k + share - 1) / share;
+            uint32_t all[W];
 #pragma unroll
-            for (int w = 0; w < W; ++w) bound = max(bound, L.wave[w]);
+            for (int w = 0; w < W; ++w) all[w] = L.first[w];
+            bound = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                int as_good = 0;
+#pragma unroll
+                for (int q = 0; q < W; ++q) as_good += all[q] >= all[w];
+                if (as_good >= waves) bound = max(bound, all[w]);
+            }
         }
         least = below(bound);
     }
@@ -271,23 +286,14 @@ struct Selection {
             hot[u] = __ballot(!(lm[u] <= least) && j + u * kT < end);
             mine += __popcll(hot[u]);
         }
-        int at = n, all = n + mine;
-        if constexpr (W > 1) {
-            if (mine) {
-                int from = 0;
-                if (lane_id() == 0) from = atomicAdd(&L.add[turn % 3], mine);
-                at += __builtin_amdgcn_readfirstlane(from);
-            }
-            __syncthreads();
-            all = n + L.add[turn % 3];
-            if (threadIdx.x == 0) L.add[(turn + 2) % 3] = 0;  // the tile's before this one
-        }
+        int at = n;
+        const int all = n + mine;
         if (all <= Lds::kKeep) {
             if (mine) {
 #pragma unroll
                 for (int u = 0; u < kTileVecs; ++u) {
                     if (hot[u] >> lane_id() & 1)
-                        L.c[at + lanes_below(hot[u])] =
+                        kept(L)[at + lanes_below(hot[u])] =
                             candidate(rank_key<DT>(lm[u]), (uint32_t)(j + u * kT));
                     at += __popcll(hot[u]);
                 }
@@ -302,21 +308,66 @@ struct Selection {
                 where[u] = (uint32_t)(j + u * kT);
                 key[u] = j + u * kT < end ? rank_key<DT>(lm[u]) : 0;
             }
-            bound = keep_best<DT, W, Lds::kKeep>(L, n, key, where, k, at_bits).key;
-            n = L.n;
+            int &held = L.held[Team<W>::wave()];
+            bound = keep_best<DT, 1, Lds::kKeep>(kept(L), held, n, key, where, k, at_bits).key;
+            n = held;
             least = logit_of<DT>(bound);
         }
     }
 
+    // The vectors that the waves have kept and that pass the best of their bounds, in
+    // the first places of L, as many as have room; every wave's n and bound are the
+    // team's then.
+    __device__ __forceinline__ void gather(Lds &L, int k, int at_bits) {
+        static_assert(W == 1 || Lds::kKeep == kT, "a wave's vectors, one a thread");
+        if (lane_id() == 0) {
+            L.held[Team<W>::wave()] = n;
+            L.last[Team<W>::wave()] = bound;
+        }
+        const int t = threadIdx.x;
+        if (t == 0) L.n = 0;
+        __syncthreads();
+        uint32_t key[W], at[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) bound = max(bound, L.last[w]);
+        int mine = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const uint64_t c = L.c[w * Lds::kKeep + t];
+            key[w] = t < L.held[w] && key_of(c) >= bound ? key_of(c) : 0;
+            at[w] = index_of(c);
+            mine += __popcll(__ballot(key[w] > 0));
+        }
+        if (lane_id() == 0) atomicAdd(&L.n, mine);
+        __syncthreads();
+        n = L.n;
+        Bound b = {0, 0};
+        if (n > Lds::kTop) b = kth_best<DT, W, W>(key, at, k, at_bits);
+        bound = max(bound, b.key);
+        __syncthreads();
+        if (t == 0) L.n = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (key[w] > 0 && passes(b, key[w], at[w])) push(L, key[w], at[w]);
+        __syncthreads();
+        n = L.n;
+    }
+
     // L holds the elements of the vectors left that may be the part's k best, few
-    // enough to be ranked
+    // enough to be ranked.  The row's tail, whose elements stand behind all others,
+    // comes in here: in a bound it would shut out equal ones before it.
     __device__ __forceinline__ void finish(Lds &L, const char *row, int full, int rem, int k,
                                            int at_bits) {
         const uint32_t none[1] = {0};
-        Team<W>::sync();
-        if (n > Lds::kTop) {
-            bound = keep_best<DT, W, Lds::kKeep>(L, n, none, none, k, at_bits).key;
-            n = L.n;
+        if constexpr (W == 1) {
+            Team<W>::sync();
+            if (n > Lds::kTop) {
+                bound = keep_best<DT, W, Lds::kKeep>(L.c, L.n, n, none, none, k, at_bits).key;
+                n = L.n;
+            }
+        } else {
+            gather(L, k, at_bits);
         }
         constexpr int kHas = (Lds::kTop + kT - 1) / kT;
         static_assert(kHas == 1, "a vector a thread");
@@ -325,32 +376,29 @@ struct Selection {
         Team<W>::sync();
         if (t == 0) L.n = 0;
         Team<W>::sync();
+        const uint32_t from = max(bound, 1u);
         if (t < n) {
-            const uint32_t from = max(bound, 1u);
-            if (j < full) {
-                float x[kV];
-                unpack<DT>(load16(row + (int64_t)j * 16), x);
-                uint32_t r[kV];
-                int mine = 0;
+            float x[kV];
+            unpack<DT>(load16(row + (int64_t)j * 16), x);
+            uint32_t r[kV];
+            int mine = 0;
 #pragma unroll
-                for (int e = 0; e < kV; ++e) {
-                    r[e] = rank_key<DT>(x[e]);
-                    mine += r[e] >= from;
-                }
-                int at = atomicAdd(&L.n, mine);
-#pragma unroll
-                for (int e = 0; e < kV; ++e)
-                    if (r[e] >= from) L.c[at++] = candidate(r[e], (uint32_t)j * kV + e);
-            } else {
-#pragma unroll 1
-                for (int e = 0; e < rem; ++e) {
-                    const uint32_t r = rank_key<DT>(load1<DT>(row, (int64_t)j * kV + e));
-                    if (r >= from) push(L, r, (uint32_t)j * kV + e);
-                }
+            for (int e = 0; e < kV; ++e) {
+                r[e] = rank_key<DT>(x[e]);
+                mine += r[e] >= from;
             }
+            int at = atomicAdd(&L.n, mine);
+#pragma unroll
+            for (int e = 0; e < kV; ++e)
+                if (r[e] >= from) L.c[at++] = candidate(r[e], (uint32_t)j * kV + e);
+        }
+        if (t < rem) {
+            const uint32_t at = (uint32_t)full * kV + t, r = rank_key<DT>(load1<DT>(row, at));
+            if (r >= from) push(L, r, at);
         }
         Team<W>::sync();
-        if (L.n > Lds::kRanked) keep_best<DT, W, Lds::kCand>(L, L.n, none, none, k, at_bits + 3);
+        if (L.n > Lds::kRanked)
+            keep_best<DT, W, Lds::kCand + kT>(L.c, L.n, L.n, none, none, k, at_bits + 3);
     }
 };
 
@@ -462,7 +510,7 @@ __global__ __launch_bounds__(kBlock, 6) void k_logprobs(LogprobArgs p) {
         Tile tile = load_tile<DT, W>(row, j, end);
         const float tail = tail_elem<DT, W>(row, full, rem);
         if (rem > 0) add_elem<true>(tail, p.c, t);
-        if constexpr (TOP) sel.start(top, tail, full, rem);
+        if constexpr (TOP) sel.start();
         for (int turn = 0; j < end; ++turn, j += kStep) {
             const Tile now = tile;
             if (j + kStep < end) tile = load_tile<DT, W>(row, j + kStep, end);
@@ -616,6 +664,19 @@ namespace {
 int64_t most_parts(int32_t top) {
     return top > 0 ? std::min<int64_t>(kMostParts, kJoin / top) : kMostParts;
 }
+// Blocks for `work` items of a team each, of `vecs` vectors, six blocks to a compute
+// unit at once.  Items that are up to half more than fit would leave most of the card
+// idle behind the first: two to a team then, where that deals the blocks evenly and an
+// item is long (2,048 rows of 131,072: 102 us, then 95; 8,192 of 32,768 with 5
+// alternatives, a wave each: 140, then 130; but 2,040 of 40,000, five tiles long, 51,
+// then 55, and 2,300 of 50,257, four and a half blocks a unit, 42, then 48).
+unsigned blocks_in_turns(int64_t work, int per_block, int64_t vecs) {
+    const int64_t fit = 6 * 256 * per_block, two = cdiv(work, 2 * per_block);
+    const bool even = cdiv(two, 256) * 256 - two <= two / 16;
+    const bool lengthy = vecs >= 8 * kTileVecs * (kBlock / per_block);
+    if (work > fit && work <= fit + fit / 2 && even && lengthy) return (unsigned)two;
+    return blocks_for(work, per_block);
+}
 }  // namespace
 
 extern "C" int pdb_token_logprobs_workspace_bytes(int64_t n, int64_t v, int32_t top,
@@ -654,7 +715,8 @@ extern "C" int pdb_token_logprobs(const void *logits, int dtype, int64_t ldz, in
                                reinterpret_cast<uint32_t *>(
                                    static_cast<char *>(ws) + stat_bytes(std::min(n, kWantBlocks)))};
         const bool wave = wave_rows(cut, n, v, kV, top > 0) && top <= TopLds<1>::kTop;
-        const unsigned blocks = blocks_for(n * cut.parts, wave ? Team<1>::kPerBlock : 1);
+        const unsigned blocks =
+            blocks_in_turns(n * cut.parts, wave ? Team<1>::kPerBlock : 1, cut.vecs);
         if (wave && top > 0)
             k_logprobs<DT, 1, true><<<blocks, kBlock, 0, s>>>(p);
         else if (wave)
