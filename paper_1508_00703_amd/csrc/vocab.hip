@@ -360,6 +360,7 @@ struct Selection {
     __device__ __forceinline__ void finish(Lds &L, const char *row, int full, int rem, int k,
                                            int at_bits) {
         const uint32_t none[1] = {0};
+        const float tail = tail_elem<DT, W>(row, full, rem);  // asked for now
         if constexpr (W == 1) {
             Team<W>::sync();
             if (n > Lds::kTop) {
@@ -393,8 +394,8 @@ struct Selection {
                 if (r[e] >= from) L.c[at++] = candidate(r[e], (uint32_t)j * kV + e);
         }
         if (t < rem) {
-            const uint32_t at = (uint32_t)full * kV + t, r = rank_key<DT>(load1<DT>(row, at));
-            if (r >= from) push(L, r, at);
+            const uint32_t r = rank_key<DT>(tail);
+            if (r >= from) push(L, r, (uint32_t)full * kV + t);
         }
         Team<W>::sync();
         if (L.n > Lds::kRanked)
