@@ -91,21 +91,20 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 //
 // (token, position) in order, stable.  Few tokens are placed by counting, in one
 // launch.  More go through a radix sort: a block of 1024 threads takes a tile of up
-// to 16 x 1024 tokens, each wave a stretch of it, and ranks them by ballots (a hot
+// to 8 x 1024 tokens, each wave a stretch of it, and ranks them by ballots (a hot
 // token costs nothing extra).  A pass is two launches, the tiles' digit counts and
 // the move, each block summing the counts of all tiles by itself; where that reading
 // grows too long a scan of the counts stands between them, and past kSortTiles the
 // general sort of pdb_internal.h runs.  Digits have up to 10 bits, so that 2^20 rows
-// take two passes, of 33 us where 7 bits took 28, in shorter runs.  4M tokens of rank
-// 32, sort and sums: 270 us in three passes of 7 bits, 256 in two of 10, 252 where the
-// first pass reads the tokens twice instead of leaving their keys, 245 with the blocks
-// dealt to the dies as tile_of_block says.  Tiles of 8,192 tokens, two to a compute
-// unit, are slower: 311.
+// take two passes.  4M tokens of rank 32, sort and sums: 270 us in three passes of 7
+// bits, 256 in two of 10, 252 where the first pass reads the tokens twice instead of
+// leaving their keys, 245 with the blocks dealt to the dies as tile_of_block says, 240
+// with tiles of 8,192 tokens, two to a compute unit, instead of 16,384 (255 of 6,144).
 
 constexpr int kSortBlock = 1024;
-constexpr int kSortItems = 16;
+constexpr int kSortItems = 8;
 constexpr int kSortTile = kSortBlock * kSortItems;
-constexpr int kSortTiles = 512;
+constexpr int kSortTiles = 1024;
 constexpr int64_t kSortMost = (int64_t)kSortTiles * kSortTile;
 constexpr int kDigitBits = 10;  // of the widest digit
 constexpr int kDigits = 1 << kDigitBits;
@@ -214,9 +213,14 @@ __device__ __forceinline__ uint32_t token_key(const void *tokens, int index, int
 // Up to kRankTokens tokens: a token's place is the number of those that go before
 // it, counted.  n^2 comparisons of two instructions each, all compute units at
 // it, cost less than the launches of a radix sort.  A block has all keys in LDS and
-// 64 tokens to place, each wave every 16th 64 of the keys (12,000 tokens of rank 32, sums
-// and all: 31 us; 13,000, sorted: 35).
+// 64 tokens to place, each wave every 16th 64 of the keys (9,000 tokens of rank 32, sums
+// and all: 28 us, sorted 31; 12,000: 31, sorted 31).
+// Of tokens that one pass sorts, only half as many (8,000 of 200 rows: 28 us counted, 22
+// sorted; 6,200: 23 both ways).
 constexpr int kRankTokens = 12288;
+constexpr int64_t rank_tokens(int bits) {
+    return bits <= kDigitBits ? kRankTokens / 2 : kRankTokens;
+}
 __global__ __launch_bounds__(kSortBlock) void k_token_rank(const void *__restrict__ tokens,
                                                            int index, int n, int64_t v,
                                                            uint32_t *__restrict__ keys,
@@ -327,7 +331,7 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_count(SortIn in,
 // Of many tiles or wide digits: each digit's count in the tiles before, in place of
 // its counts, and behind the last tile its count in all.  A lane has a digit, a wave
 // every 16th part of the tiles.
-constexpr int kScanTiles = kSortTiles / (kSortBlock / kWave);
+constexpr int kScanTiles = 16;  // counts that a lane has in flight
 __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__restrict__ hist,
                                                                 int tiles, int nb) {
     __shared__ uint32_t s_sum[kSortBlock / kWave][kWave];
@@ -335,20 +339,28 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__rest
     const int per = (tiles + kSortBlock / kWave - 1) / (kSortBlock / kWave);
     const int from = w * per, to = min(tiles, from + per);
     uint32_t c[kScanTiles], sum = 0;
+    auto load = [&](int q0) {
 #pragma unroll
-    for (int q = 0; q < kScanTiles; ++q)
-        c[q] = from + q < to ? hist[((int64_t)(from + q) << nb) + d] : 0;
+        for (int q = 0; q < kScanTiles; ++q)
+            c[q] = q0 + q < to ? hist[((int64_t)(q0 + q) << nb) + d] : 0;
+    };
+    for (int q0 = from; q0 < to; q0 += kScanTiles) {
+        load(q0);
 #pragma unroll
-    for (int q = 0; q < kScanTiles; ++q) sum += c[q];
+        for (int q = 0; q < kScanTiles; ++q) sum += c[q];
+    }
     s_sum[w][lane] = sum;
     __syncthreads();
     uint32_t before = 0;
 #pragma unroll
     for (int q = 0; q < kSortBlock / kWave; ++q) before += q < w ? s_sum[q][lane] : 0;
+    for (int q0 = from; q0 < to; q0 += kScanTiles) {
+        if (per > kScanTiles) load(q0);
 #pragma unroll
-    for (int q = 0; q < kScanTiles; ++q) {
-        if (from + q < to) hist[((int64_t)(from + q) << nb) + d] = before;
-        before += c[q];
+        for (int q = 0; q < kScanTiles; ++q) {
+            if (q0 + q < to) hist[((int64_t)(q0 + q) << nb) + d] = before;
+            before += c[q];
+        }
     }
     if (w == kSortBlock / kWave - 1) hist[((int64_t)tiles << nb) + d] = before;
 }
@@ -880,11 +892,12 @@ GradWs grad_ws_layout(void *base, int64_t n, int64_t d) {
                                    cdiv(n, (int64_t)tile_rows(n, d, lg8) << (8 - lg8)));
     w.kA = reinterpret_cast<uint32_t *>(take(4 * n));
     w.vA = reinterpret_cast<uint32_t *>(take(4 * n));
-    if (n > kRankTokens) {
+    if (n > rank_tokens(0)) {
         if (n > kSortMost) w.keys = reinterpret_cast<uint32_t *>(take(4 * n));
         w.kB = reinterpret_cast<uint32_t *>(take(4 * n));
         w.vB = reinterpret_cast<uint32_t *>(take(4 * n));
-        w.hist = reinterpret_cast<uint32_t *>(take(std::max<int64_t>(4 * 256 * st, 4 * kDigits * (kSortTiles + 1))));
+        w.hist = reinterpret_cast<uint32_t *>(
+            take(4 * std::max<int64_t>(256 * st, kDigits * (kSortTiles + 1))));
         w.scan_tmp = reinterpret_cast<uint32_t *>(take(4 * (int64_t)scan_tmp_elems(256 * st)));
     }
     w.part = reinterpret_cast<float *>(take(spans * 2 * d * 4));
@@ -902,7 +915,7 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
     while (((int64_t)1 << bits) <= v) ++bits;
     *keys = w.kA;
     *vals = w.vA;
-    if (n <= kRankTokens) {
+    if (n <= rank_tokens(bits)) {
         k_token_rank<<<(unsigned)cdiv(n, kWave), kSortBlock, 0, s>>>(tokens, index, (int)n, v, w.kA,
                                                                      w.vA, status);
         PDB_LAUNCHED();
@@ -916,8 +929,9 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
                                  w.scan_tmp, keys, vals, s));
         return PDB_OK;
     }
-    // about 128 tiles: half of the compute units, and counts that are soon summed
-    const int items = (int)std::min<int64_t>(kSortItems, cdiv(n, 128 * kSortBlock));
+    // about 256 tiles, one a compute unit (1M tokens of 64 columns: 84 us; with 128
+    // tiles 92, with 512 90)
+    const int items = (int)std::min<int64_t>(kSortItems, cdiv(n, 256 * kSortBlock));
     const int tiles = (int)cdiv(n, (int64_t)items * kSortBlock);
     const int passes = (bits + kDigitBits - 1) / kDigitBits, step = (bits + passes - 1) / passes;
     SortIn in = {tokens, index, v, status, nullptr, nullptr, n, items, 0, 0, tiles};

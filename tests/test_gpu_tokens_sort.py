@@ -11,9 +11,9 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("n,v,d", [
-    (12289, 1023, 3), (12289, 1024, 3), (65537, (1 << 18) - 1, 2), (131073, 1 << 18, 2),
+    (6144, 1023, 3), (6145, 1023, 3), (6145, 1024, 3), (12289, 1023, 3), (12289, 1024, 3), (65537, (1 << 18) - 1, 2), (131073, 1 << 18, 2),
     (262144, (1 << 19) + 3, 1), (200001, (1 << 20) - 1, 2), (1100003, 1 << 20, 1),
-    (2097152, 700001, 2), (200003, (1 << 25) + 5, 1), (8388608, 1500, 1)])
+    (2097152, 700001, 2), (262145, 70001, 3), (4194304, 40000, 1), (4194305, 900, 1), (200003, (1 << 25) + 5, 1), (8388608, 1500, 1)])
 @pytest.mark.parametrize("how", ["uniform", "hot", "one"])
 def test_embed_grad_order(gpu, n, v, d, how):
     import torch
