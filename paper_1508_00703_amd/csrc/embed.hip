@@ -694,9 +694,10 @@ __global__ __launch_bounds__(kBlock) void k_embed_tiles(GradArgs p) {
 // entry holds the token (slots and first entries are read together: waiting for one
 // to know whether to read the other would double the trips).  A run of more than
 // kOwn spans is added by the whole block, every group each G-th span and then the
-// groups' sums pairwise.  Groups are narrow, 16 lanes at most, so that a hot
-// token's run is spread over many of them.
-constexpr int kJoinBlock = 512, kJoinLg = 4;
+// groups' sums pairwise.  Groups are narrow, 8 lanes where rows are not wider than a
+// grid, so that a hot token's run is spread over many of them (3M tokens of 32 columns,
+// Zipf: 145 us, with 16 lanes of blocks twice as large 151).
+constexpr int kJoinBlock = 256, kJoinLg = 3;
 template <int GT, int E, bool ACC>
 __global__ __launch_bounds__(kJoinBlock) void k_embed_join(GradArgs p) {
     constexpr int kJoinAhead = 32 / E, kOwn = 4 * kJoinAhead;  // slots in flight; four trips
@@ -974,7 +975,7 @@ int embed_grad(GradArgs p, const GradWs &w, hipStream_t s) {
     p.zero_lg = lanes_log2(cdiv(p.d, Elem<GT>::kVec));
     p.zero_blocks = ACC ? 0 : std::min<int64_t>(cdiv(p.v, kWave), 1 << 18);
     const int64_t slices = cdiv(vectors, 1 << p.lg), per = kBlock >> p.lg;
-    if (cdiv(vectors, 1 << std::min(p.lg, kJoinLg)) > 65535) return PDB_ERR_UNSUPPORTED;
+    if (slices > 65535) return PDB_ERR_UNSUPPORTED;
     if (p.n <= kDirect) {
         p.sum_blocks = cdiv(p.n, per);
         const dim3 grid((unsigned)(p.sum_blocks + p.zero_blocks), (unsigned)slices);
@@ -995,7 +996,9 @@ int embed_grad(GradArgs p, const GradWs &w, hipStream_t s) {
     k_embed_tiles<DT, GT, ACC><<<grid, kBlock, 0, s>>>(p);
     PDB_LAUNCHED();
     if (p.sum_blocks == 1) return PDB_OK;
-    p.lg = std::min(p.lg, kJoinLg);
+    const int lg = p.lg;
+    p.lg = std::min(lg, kJoinLg);
+    while (p.lg < lg && cdiv(vectors, 1 << p.lg) > 65535) ++p.lg;
     const dim3 join((unsigned)cdiv(p.sum_blocks, kJoinBlock >> p.lg),
                     (unsigned)cdiv(vectors, 1 << p.lg));
     k_embed_join<GT, kE, ACC><<<join, kJoinBlock, 0, s>>>(p);

@@ -11,9 +11,10 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("n,v,d", [
-    (6144, 1023, 3), (6145, 1023, 3), (6145, 1024, 3), (12289, 1023, 3), (12289, 1024, 3), (65537, (1 << 18) - 1, 2), (131073, 1 << 18, 2),
-    (262144, (1 << 19) + 3, 1), (200001, (1 << 20) - 1, 2), (1100003, 1 << 20, 1),
-    (2097152, 700001, 2), (262145, 70001, 3), (4194304, 40000, 1), (4194305, 900, 1), (200003, (1 << 25) + 5, 1), (8388608, 1500, 1)])
+    (6144, 1023, 3), (6145, 1023, 3), (6145, 1024, 3), (12289, 1023, 3), (12289, 1024, 3),
+    (65537, (1 << 18) - 1, 2), (131073, 1 << 18, 2), (262144, (1 << 19) + 3, 1),
+    (200001, (1 << 20) - 1, 2), (1100003, 1 << 20, 1), (2097152, 700001, 2), (262145, 70001, 3),
+    (4194304, 40000, 1), (4194305, 900, 1), (200003, (1 << 25) + 5, 1), (8388608, 1500, 1)])
 @pytest.mark.parametrize("how", ["uniform", "hot", "one"])
 def test_embed_grad_order(gpu, n, v, d, how):
     import torch
@@ -46,3 +47,16 @@ def test_embed_grad_order(gpu, n, v, d, how):
         got = native.pdb_embed_grad(dyg, tg, torch.full((v, d), 5.0, device=gpu), status=status)
         check(f64(got), want - less, bound, "grad without it")
         assert int(status) == -1
+
+
+def test_rows_wider_than_a_grid_of_narrow_groups(gpu):
+    """Tokens that cross blocks, in rows of over 2^21 columns."""
+    import torch
+
+    native = native_mod()
+    n, v, d = 300, 3, (1 << 21) + 3
+    tok = torch.arange(n, device=gpu) * v // n
+    dy = torch.ones(n, d, device=gpu)
+    dy[:, 1::2] = 2.0
+    got = native.pdb_embed_grad(dy, tok, torch.full((v, d), 7.0, device=gpu))
+    assert torch.equal(got, dy[:v] * (n // v))
