@@ -99,7 +99,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 // take two passes.  4M tokens of rank 32, sort and sums: 270 us in three passes of 7
 // bits, 256 in two of 10, 252 where the first pass reads the tokens twice instead of
 // leaving their keys, 245 with the blocks dealt to the dies as tile_of_block says, 240
-// with tiles of 8,192 tokens, two to a compute unit, instead of 16,384 (255 of 6,144).
+// with tiles of 8,192 tokens, two to a compute unit, instead of 16,384 (255 of 6,144),
+// and 233 with today's scan and join.
 
 constexpr int kSortBlock = 1024;
 constexpr int kSortItems = 8;
@@ -329,15 +330,17 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_count(SortIn in,
 }
 
 // Of many tiles or wide digits: each digit's count in the tiles before, in place of
-// its counts, and behind the last tile its count in all.  A lane has a digit, a wave
-// every 16th part of the tiles.
+// its counts, and behind the last tile its count in all.  A block has 32 digits, half a
+// wave every 32nd part of the tiles (489 tiles of 1,024 digits: 5.0 us; a wave every 16th part of 64 digits 7.2).
+constexpr int kScanDigits = 32, kScanParts = kSortBlock / kScanDigits;
 constexpr int kScanTiles = 16;  // counts that a lane has in flight
 __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__restrict__ hist,
                                                                 int tiles, int nb) {
-    __shared__ uint32_t s_sum[kSortBlock / kWave][kWave];
-    const int w = wave_in_block(), lane = lane_id(), d = (int)blockIdx.x * kWave + lane;
-    const int per = (tiles + kSortBlock / kWave - 1) / (kSortBlock / kWave);
-    const int from = w * per, to = min(tiles, from + per);
+    __shared__ uint32_t s_sum[kScanParts][kScanDigits];
+    const int part = threadIdx.x / kScanDigits, mine = threadIdx.x % kScanDigits;
+    const int d = (int)blockIdx.x * kScanDigits + mine;
+    const int per = (tiles + kScanParts - 1) / kScanParts;
+    const int from = part * per, to = min(tiles, from + per);
     uint32_t c[kScanTiles], sum = 0;
     auto load = [&](int q0) {
 #pragma unroll
@@ -349,11 +352,11 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__rest
 #pragma unroll
         for (int q = 0; q < kScanTiles; ++q) sum += c[q];
     }
-    s_sum[w][lane] = sum;
+    s_sum[part][mine] = sum;
     __syncthreads();
     uint32_t before = 0;
 #pragma unroll
-    for (int q = 0; q < kSortBlock / kWave; ++q) before += q < w ? s_sum[q][lane] : 0;
+    for (int q = 0; q < kScanParts; ++q) before += q < part ? s_sum[q][mine] : 0;
     for (int q0 = from; q0 < to; q0 += kScanTiles) {
         if (per > kScanTiles) load(q0);
 #pragma unroll
@@ -362,7 +365,7 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__rest
             before += c[q];
         }
     }
-    if (w == kSortBlock / kWave - 1) hist[((int64_t)tiles << nb) + d] = before;
+    if (part == kScanParts - 1) hist[((int64_t)tiles << nb) + d] = before;
 }
 
 // Block b's tile: the blocks of one die (b mod 8) have neighbouring tiles, whose
@@ -946,7 +949,7 @@ int sort_tokens(const GradWs &w, const void *tokens, int index, int64_t n, int64
         PDB_LAUNCHED();
         const bool scan = nb >= 6 && (int64_t)tiles << nb > kDirectCounts;
         if (scan) {
-            k_token_sort_scan<<<1 << (nb - 6), kSortBlock, 0, s>>>(w.hist, tiles, nb);
+            k_token_sort_scan<<<(1 << nb) / kScanDigits, kSortBlock, 0, s>>>(w.hist, tiles, nb);
             PDB_LAUNCHED();
         }
         uint32_t *tk = in.keys == w.kA ? w.kB : w.kA, *tv = in.keys == w.kA ? w.vB : w.vA;
