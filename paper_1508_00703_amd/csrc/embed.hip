@@ -215,9 +215,8 @@ __device__ __forceinline__ uint32_t token_key(const void *tokens, int index, int
 // it, counted.  n^2 comparisons of two instructions each, all compute units at
 // it, cost less than the launches of a radix sort.  A block has all keys in LDS and
 // 64 tokens to place, each wave every 16th 64 of the keys (9,000 tokens of rank 32, sums
-// and all: 28 us, sorted 31; 12,000: 31, sorted 31).
-// Of tokens that one pass sorts, only half as many (8,000 of 200 rows: 28 us counted, 22
-// sorted; 6,200: 23 both ways).
+// and all: 28 us, sorted 31; 12,000: 31, sorted 31).  Of tokens that one pass sorts, only
+// half as many (8,000 of 200 rows: 28 us counted, 22 sorted; 6,200: 23 both ways).
 constexpr int kRankTokens = 12288;
 constexpr int64_t rank_tokens(int bits) {
     return bits <= kDigitBits ? kRankTokens / 2 : kRankTokens;
@@ -331,7 +330,8 @@ __global__ __launch_bounds__(kSortBlock) void k_token_sort_count(SortIn in,
 
 // Of many tiles or wide digits: each digit's count in the tiles before, in place of
 // its counts, and behind the last tile its count in all.  A block has 32 digits, half a
-// wave every 32nd part of the tiles (489 tiles of 1,024 digits: 5.0 us; a wave every 16th part of 64 digits 7.2).
+// wave every 32nd part of the tiles (489 tiles of 1,024 digits: 5.0 us; 64 digits and a
+// wave every 16th part: 7.2).
 constexpr int kScanDigits = 32, kScanParts = kSortBlock / kScanDigits;
 constexpr int kScanTiles = 16;  // counts that a lane has in flight
 __global__ __launch_bounds__(kSortBlock) void k_token_sort_scan(uint32_t *__restrict__ hist,

@@ -14,8 +14,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // path serves every base and stride.
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-__device__ __forceinline__ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 __host__ __device__ constexpr int dtype_size(int dt) { return dt == PDB_F32 ? 4 : 2; }
 
 template <int DT>
@@ -28,13 +26,6 @@ __device__ __forceinline__ u32x4 load16(const void *p) {
     return *static_cast<const u32x4_any *>(p);
 }
 __device__ __forceinline__ void store16(void *p, u32x4 v) { *static_cast<u32x4_any *>(p) = v; }
-// for bytes that this kernel touches once: they do not displace what is reused
-__device__ __forceinline__ u32x4 load16_once(const void *p) {
-    return __builtin_nontemporal_load(static_cast<const u32x4_any *>(p));
-}
-__device__ __forceinline__ void store16_once(void *p, u32x4 v) {
-    __builtin_nontemporal_store(v, static_cast<u32x4_any *>(p));
-}
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
