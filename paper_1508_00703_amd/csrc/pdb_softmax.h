@@ -5,9 +5,11 @@
 //   m = max z,  y_j = c (z_j - m),  S = sum 2^y_j,  A = sum 2^y_j y_j.
 // One pass keeps a running m per wave and rescales S and A in the rare tiles
 // that raise it (a wave's maximum is raised about ln(tiles) times), so an
-// element costs one exponential.  y is one fma on M = fl(c m): what rounding M
-// shifts is the same for every element and is taken out of log S at the end.
-// Where |M| nears the range's end (rows of a type's lowest value) y is c (z - m)
+// element costs one exponential.  y is one fma on M = fl(c m) while |M| is below
+// 2^20: what rounding M shifts, up to 2^-5, is the same for every element and is taken
+// out of log S at the end.  Where |M| is larger (masks like -1e30, a type's lowest
+// value, temperatures far below the logits) the shift would leave the exponential's
+// range, from 2^31 on, and cost the sums their accuracy before: y is c (z - m) there
 // instead.  m starts at the lowest finite float, so a logit of -inf gives 2^y = 0
 // without a special case and S = 0 says that a row has nothing else.  A takes y no
 // lower than kLogFloor, where 2^y is 0: 0 log 0 counts as 0.
@@ -83,15 +85,20 @@ __device__ __forceinline__ float wave_uniform(float v) {
     return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
 }
 
-// Whether y may be taken as c z - M.
-__device__ __forceinline__ bool in_range(float m, float c) { return fabsf(m * c) < 1e38f; }
+// Whether y is taken as c z - M, and how much larger it is than c (z - m) then.
+__device__ __forceinline__ bool in_range(float m, float c) { return fabsf(m * c) < 0x1p20f; }
+__device__ __forceinline__ float shift_of(float m, float c) {
+    return in_range(m, c) ? __builtin_fmaf(m, c, -(m * c)) : 0.0f;
+}
 __device__ __forceinline__ float power_of(float z, float m, float c) {
     return in_range(m, c) ? __builtin_fmaf(z, c, -(m * c)) : (z - m) * c;
 }
 
 // t's sums on the maximum m >= t.m
 __device__ __forceinline__ void rescale(Stat &t, float m, float c) {
-    const float up = in_range(m, c) ? t.m * c - m * c : (t.m - m) * c;
+    const float up = in_range(m, c) && in_range(t.m, c)
+                         ? t.m * c - m * c
+                         : (t.m - m) * c + (shift_of(m, c) - shift_of(t.m, c));
     const float y = fmaxf(up, 2.0f * kLogFloor);
     const float f = exp2_raw(y);
     t.a = f * __builtin_fmaf(y, t.s, t.a);
@@ -148,8 +155,7 @@ __device__ __forceinline__ void put_part(float *part_stat, int64_t w, const Stat
 // empty row, and the entropy.
 __device__ __forceinline__ float log_sum(const Stat &t, float c) {
     if (t.s == 0.0f) return kNegInf;
-    const float l = __builtin_amdgcn_logf(t.s);
-    return (in_range(t.m, c) ? l - __builtin_fmaf(t.m, c, -(t.m * c)) : l) * kLn2;
+    return (__builtin_amdgcn_logf(t.s) - shift_of(t.m, c)) * kLn2;
 }
 __device__ __forceinline__ float entropy_of(const Stat &t) {
     return t.s == 0.0f ? 0.0f : (__builtin_amdgcn_logf(t.s) - t.a / t.s) * kLn2;
