@@ -124,11 +124,13 @@ int pdb_distill_workspace_bytes(int64_t n, int64_t v, size_t *bytes);
  * top_id and top_logp are such: any logits that differ from the teacher's by a
  * constant per row serve); a negative id is no entry.  weight: device, [n], or
  * NULL for ones.  temp > 0 and finite.  A row without entries (or whose
- * entries' teacher logits are all -inf), or of weight 0, is not read: loss 0,
- * gradient 0.  A logit of -inf where p > 0 makes the loss +inf (the gradient
- * stays finite).  dlogits: device, n x v, row stride ldd, of the logits' type;
- * it may be the logits themselves (same pointer and row stride).  status as for
- * tokens, for ids >= v.  ws: at least pdb_distill_workspace_bytes(n, v). */
+ * entries' teacher logits are all -inf), or of weight 0, has loss 0 and
+ * gradient 0 whatever its logits; the ids of a row of weight 0 may hold
+ * anything.  A logit of -inf where p > 0 makes the loss +inf (the gradient stays
+ * finite).  dlogits: device, n x v, row stride ldd, of the logits' type; it may
+ * be the logits themselves (same pointer and row stride).  status as for
+ * tokens, for ids >= v in rows of other weights.  ws: at least
+ * pdb_distill_workspace_bytes(n, v). */
 int pdb_distill(const void *logits, int dtype, int64_t ldz, int64_t n, int64_t v,
                 const int32_t *ids, const void *teacher, int teacher_dtype, int32_t k, float temp,
                 const float *weight, float *loss, void *dlogits, int64_t ldd, int32_t *status,

@@ -50,7 +50,9 @@ __device__ __forceinline__ float load_teacher(const DistillArgs &p, int64_t at) 
                                        : load1<PDB_F16>(p.teacher, at);
 }
 
-// One wave fills L; the others see it after the team's next barrier.
+// One wave fills L; the others see it after the team's next barrier.  An id out of range
+// is noted unless the row's weight is 0: such rows come here too where others' loads are
+// under way (to leave them out took 38.2 -> 39.6 us for 4,200 rows of 8,000 bf16).
 template <int DT, int K>
 __device__ __forceinline__ void teacher_row(const DistillArgs &p, int64_t i, const char *row,
                                             TeacherLds<K> &L) {
@@ -59,7 +61,7 @@ __device__ __forceinline__ void teacher_row(const DistillArgs &p, int64_t i, con
     for (int j = lane_id(); j < p.k; j += kWave) {
         int32_t id = p.ids[i * p.k + j];
         if (id >= p.v) {
-            if (p.status) *p.status = PDB_ERR_INVALID_ARG;
+            if (p.status && row_weight(p, i) != 0.0f) *p.status = PDB_ERR_INVALID_ARG;
             id = -1;
         }
         const float y = id < 0 ? kNegInf : load_teacher(p, i * p.k + j);
