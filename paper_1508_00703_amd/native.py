@@ -633,19 +633,23 @@ def _raw_stream(stream, device):
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _empty(like, shape, dtype, stream):
-    """A new tensor on like's device, kept from reuse until the stream, where it is
-    not the current one, is done with it."""
-    t = torch.empty(shape, dtype=dtype, device=like.device)
-    if stream is not None:
-        t.record_stream(stream)
+def _empty(like, shape, dtype, stream, returned=True):
+    """A new tensor on like's device, from the memory of the stream that the call runs on:
+    what another stream's allocations have freed, that stream may still be reading.  One
+    that is returned is kept from reuse until the current stream, too, is done with it."""
+    if stream is None or stream.cuda_stream == _raw_stream(None, like.get_device()):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(like.device))
     return t
 
 
 def _space(ws, nbytes, like, stream):
     """(address, bytes) of the given workspace or of a new one, and that tensor."""
     if ws is None:
-        ws = _empty(like, nbytes, torch.uint8, stream)
+        ws = _empty(like, nbytes, torch.uint8, stream, returned=False)
     elif ws.get_device() != like.get_device() or not ws.is_contiguous():
         raise ValueError("ws must be contiguous and on the other tensors' device")
     return ws.data_ptr(), ws.numel(), ws

@@ -33,3 +33,47 @@ def test_ids_of_a_row_of_weight_0(gpu, n, v, dtype):
         status.zero_()
         native.pdb_distill(z, ids, t, weight=w, grad=grad, status=status)
         assert int(status) == native.PDB_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("n,v", [(3, 20011), (1000, 1500)])
+def test_memory_freed_by_a_busy_stream(gpu, n, v):
+    """The current stream has freed blocks of just the sizes that the call wants and has
+    yet to read them: a call on another stream leaves them alone."""
+    import torch
+
+    native = native_mod()
+    z = torch.randn(n, v, device=gpu)
+    tok = torch.randint(0, v, (n,), device=gpu)
+    ids = torch.randint(0, v, (n, 8), device=gpu, dtype=torch.int32)
+    t, g = torch.randn(n, 8, device=gpu), torch.randn(n, device=gpu)
+    w, dy = torch.randn(v, 24, device=gpu), torch.randn(n, 24, device=gpu)
+    grad = torch.empty(v, 24, device=gpu)
+    a = torch.randn(4096, 4096, device=gpu)
+    sizes = [native.pdb_token_logprobs_workspace_bytes(n, v, 20), native.pdb_distill_workspace_bytes(n, v),
+             native.pdb_embed_grad_workspace_bytes(n, v, 24), 4 * n, 8 * n, 80 * n, 96 * n, 4 * n * v]
+
+    def calls(stream):
+        f = native.pdb_token_logprobs(z, tok, top=20, stream=stream)
+        d = native.pdb_token_logprobs_grad(z, tok, f.stats, g, f.entropy, g, stream=stream)
+        loss, e = native.pdb_distill(z, ids, t, stream=stream)
+        out = native.pdb_embed_lookup(w, tok, stream=stream)
+        return [f.logp, f.entropy, f.top_id, f.top_logp, d, loss, e, out,
+                native.pdb_embed_grad(dy, tok, grad, stream=stream)]
+
+    want = [x.clone() for x in calls(None)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        blocks = [torch.full((s,), 7, dtype=torch.uint8, device=gpu) for s in sizes for _ in range(3)]
+        torch.cuda.synchronize()
+        for _ in range(8):  # some milliseconds of work ahead of the reading
+            b = a @ a
+        seen = [x.clone() for x in blocks]
+        del blocks
+        got = calls(side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(bool((x == 7).all()) for x in seen)
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+        del b, seen, got
