@@ -657,12 +657,15 @@ def _space(ws, nbytes, like, stream):
 
 def _on_own_device(call):
     """Runs a call with its first tensor's device as the current one."""
+    name = call.__code__.co_varnames[0]
+
     @functools.wraps(call)
-    def run(first, *args, **kw):
-        if first.is_cuda and first.get_device() != torch._C._cuda_getDevice():
+    def run(*args, **kw):
+        first = args[0] if args else kw.get(name)
+        if first is not None and first.is_cuda and first.get_device() != torch._C._cuda_getDevice():
             with torch.cuda.device(first.device):
-                return call(first, *args, **kw)
-        return call(first, *args, **kw)
+                return call(*args, **kw)
+        return call(*args, **kw)
     return run
 
 

@@ -77,3 +77,23 @@ def test_memory_freed_by_a_busy_stream(gpu, n, v):
         for x, y in zip(got, want):
             assert torch.equal(x, y)
         del b, seen, got
+
+
+def test_arguments_by_name(gpu):
+    import torch
+
+    native = native_mod()
+    w, tok = torch.randn(30, 8, device=gpu), torch.randint(0, 30, (5,), device=gpu)
+    z, g = torch.randn(5, 30, device=gpu), torch.randn(5, device=gpu)
+    ids = tok[:, None].int().contiguous()
+    x = native.pdb_embed_lookup(table=w, tokens=tok)
+    assert torch.equal(x, w[tok])
+    assert torch.equal(native.pdb_embed_grad(dy=x, tokens=tok, grad=torch.empty_like(w)),
+                       native.pdb_embed_grad(x, tok, torch.empty_like(w)))
+    f = native.pdb_token_logprobs(logits=z, tokens=tok)
+    assert torch.equal(f.logp, native.pdb_token_logprobs(z, tok).logp)
+    assert torch.equal(native.pdb_token_logprobs_grad(logits=z, tokens=tok, stats=f.stats, d_logp=g),
+                       native.pdb_token_logprobs_grad(z, tok, f.stats, g))
+    for a, b in zip(native.pdb_distill(logits=z, ids=ids, teacher=g[:, None]),
+                    native.pdb_distill(z, ids, g[:, None])):
+        assert torch.equal(a, b)

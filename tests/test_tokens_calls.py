@@ -73,3 +73,24 @@ def test_memory_comes_from_the_stream_of_the_call(native, streams):
         assert home is current or out.recorded == [current]
         _, _, ws = native._space(None, 100, Like(), stream)
         assert ws.home is home
+
+
+CALLS = {
+    "pdb_embed_lookup": ("table", "tokens"),
+    "pdb_embed_grad": ("dy", "tokens", "grad"),
+    "pdb_token_logprobs": ("logits",),
+    "pdb_token_logprobs_grad": ("logits", "tokens", "stats"),
+    "pdb_distill": ("logits", "ids", "teacher"),
+}
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_every_argument_by_name(native, call):
+    """The arguments are taken (and then refused, for they are on no device); one that is
+    missing is named."""
+    given = {name: torch.zeros(3, 10) for name in CALLS[call]}
+    with pytest.raises(ValueError, match="device"):
+        getattr(native, call)(**given)
+    for name in given:
+        with pytest.raises(TypeError, match="'%s'" % name):
+            getattr(native, call)(**{k: x for k, x in given.items() if k != name})
