@@ -133,3 +133,21 @@ def test_the_lowest_value_at_any_temperature(gpu, n, v, dtype, temp):
     # a teacher under the same mask proposes none of its entries
     ids = np.repeat(z64.argmax(axis=1).astype(np.int32)[:, None], 2, axis=1)
     check_distill(gpu, rng, z, z64, ids, rng.normal(size=(n, 2)), temp, dtype)
+
+
+@pytest.mark.parametrize("n,v", SIZES)
+@pytest.mark.parametrize("temp", [1.0, 0.7, 3.0])
+@pytest.mark.parametrize("side", [-1, 1])
+def test_rows_across_the_two_forms(gpu, n, v, temp, side):
+    """The running maximum passes |log2(e) m / T| = 2^20, where the sums go from one form
+    of their powers to the other, while both sides count: rising, falling, in any order."""
+    rng = np.random.default_rng(n + v + 4)
+    edge = side * 2.0 ** 20 * np.log(2.0) * temp
+    z = np.broadcast_to(np.linspace(-6.0, 6.0, v) * temp, (n, v)).copy()
+    z[1::3] = z[1::3, ::-1]
+    z[2::3] = rng.permuted(z[2::3], axis=1)
+    z += rng.uniform(-5.0, 5.0, (n, 1)) * temp + edge
+    z, z64 = on_gpu(z, "f32", gpu)
+    check_scores(gpu, rng, z, z64, temp, "f32")
+    ids = rng.integers(0, v, (n, 8)).astype(np.int32)
+    check_distill(gpu, rng, z, z64, ids, edge + rng.normal(size=(n, 8)), temp, "f32")
