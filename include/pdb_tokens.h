@@ -21,8 +21,9 @@
  * call here does, so one word can watch many calls.
  *
  * Arithmetic: binary32 whatever the types, rounded once (to nearest even) where
- * a 16-bit result is stored.  Every sum runs in an order that the sizes alone
- * fix, so a repeated call gives the same bits.
+ * a 16-bit result is stored; what passes its type's range is infinite.  The
+ * order of every sum follows from the call's sizes and, in pdb_embed_grad, from
+ * all of its tokens, so a repeated call gives the same bits.
  */
 #ifndef PDB_TOKENS_H
 #define PDB_TOKENS_H
@@ -63,9 +64,10 @@ int pdb_embed_grad_workspace_bytes(int64_t n, int64_t v, int64_t d, size_t *byte
  * table itself and scale = -lr times the lookup's scale that is the gradient
  * step of Sec. 2 on the rows that the batch used (Definition 3: every read of
  * the batch before its writes).  grad: device, v x d, row stride ldg, of
- * grad_dtype.  A token's rows are summed in ascending i, in runs that the sizes
- * fix, then the runs' sums.  ws: at least
- * pdb_embed_grad_workspace_bytes(n, v, d). */
+ * grad_dtype.  A token's rows are summed in ascending i, in runs, then the runs'
+ * sums.  Where the runs end depends on how many rows the smaller tokens have: a
+ * row's last bits may differ between batches that differ in other tokens only.
+ * ws: at least pdb_embed_grad_workspace_bytes(n, v, d). */
 int pdb_embed_grad(const void *dy, int dtype, int64_t ldy, const void *tokens, int index,
                    int64_t n, void *grad, int grad_dtype, int64_t ldg, int64_t v, int64_t d,
                    float scale, int accumulate, int32_t *status, void *ws, size_t ws_bytes,

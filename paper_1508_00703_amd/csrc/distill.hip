@@ -7,8 +7,10 @@
 // twice -- unless a row stays on chip.  It does in registers: 16 vectors a thread, as
 // they are stored, with one to sixteen waves to a row, which holds rows of up to
 // 131,072 16-bit logits and leaves 16 waves on every compute unit.  The floor is then
-// one read and one write.  Longer rows, and rows too few to fill the card, go the
-// other way: a kernel for the statistics of their parts and one for the gradient.
+// one read and one write (4,096 rows of 131,072 bf16: 436 us, 4.9 TB/s).  Longer rows,
+// and rows too few to fill the card, go the other way: a kernel for the statistics of
+// their parts and one for the gradient (1,024 rows of 151,936 bf16: 210 us, 94 and 114,
+// where one read and one write would be 121; of 262,144: 337; 64 rows of 131,072: 20).
 #include "pdb_softmax.h"
 
 namespace pdbk {

@@ -13,8 +13,9 @@
 // hot token's rows are then spread over many groups and a rare token costs one
 // row.  A token whose entries lie in one tile is written by that tile; the
 // parts of one that crosses tiles go to a partial buffer and are joined in
-// tile order by a second kernel.  No atomics: the order of every sum follows
-// from the sizes.
+// tile order by a second kernel.  No atomics on sums: their order follows from the
+// sizes and from where the tiles cut the sorted tokens, and is the same in every call
+// on the same tokens.
 #include "pdb_vec.h"
 
 namespace pdbk {
@@ -94,13 +95,14 @@ __global__ __launch_bounds__(kBlock) void k_embed_lookup(const void *__restrict_
 // to 8 x 1024 tokens, each wave a stretch of it, and ranks them by ballots (a hot
 // token costs nothing extra).  A pass is two launches, the tiles' digit counts and
 // the move, each block summing the counts of all tiles by itself; where that reading
-// grows too long a scan of the counts stands between them, and past kSortTiles the
-// general sort of pdb_internal.h runs.  Digits have up to 10 bits, so that 2^20 rows
-// take two passes.  4M tokens of rank 32, sort and sums: 270 us in three passes of 7
-// bits, 256 in two of 10, 252 where the first pass reads the tokens twice instead of
-// leaving their keys, 245 with the blocks dealt to the dies as tile_of_block says, 240
-// with tiles of 8,192 tokens, two to a compute unit, instead of 16,384 (255 of 6,144),
-// and 233 with today's scan and join.
+// grows too long a scan of the counts stands between them.  Digits have up to 10 bits,
+// so that 2^20 rows take two passes.  4M tokens of rank 32, sort and sums: 270 us in
+// three passes of 7 bits, 256 in two of 10, 252 where the first pass reads the tokens
+// twice instead of leaving their keys, 245 with the blocks dealt to the dies as
+// tile_of_block says, 240 with tiles of 8,192 tokens, two to a compute unit, instead of
+// 16,384 (255 of 6,144), and 233 with today's scan and join.  Past kSortTiles, where the
+// counts would outgrow their place, the general sort of pdb_internal.h runs (8,388,608
+// tokens of rank 32: 415 us, 146 of them sorting; 8.4M so: 531; 20M: 1,065, 495 sorting).
 
 constexpr int kSortBlock = 1024;
 constexpr int kSortItems = 8;

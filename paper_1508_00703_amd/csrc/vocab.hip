@@ -19,10 +19,10 @@ namespace {
 // by (largest key, index): an element of any other has K better ones.  So while a
 // row streams by, only its vectors' maxima are looked at: those better than a bound
 // are kept in LDS, by each wave in a place of its own, so that the waves of a team
-// wait for each other at a row's ends only (with a barrier every tile, 1,000 rows of
-// 100,003 in 32 bits took 90 us with 64 alternatives, now 83).  The bound is the K-th
-// best of K or more vectors met so far.  The first tile sets it, from the K-th best of
-// a wave's vectors, or from the (K / W)-th best of each of W waves'; when a wave's
+// wait for each other at a row's ends only (of 1,000 rows of 100,003 in 32 bits with 64
+// alternatives, 89 us, a barrier every tile took 7 more).  The bound is the K-th best of
+// K or more vectors met so far.  The first tile sets it, from the K-th best of a wave's
+// vectors, or from the (K / W)-th best of each of W waves'; when a wave's
 // kept ones would overflow, its bound is raised to the K-th best of those kept and the
 // tile's, which leaves K, whatever the data.  Of the vectors kept in the end the K best
 // are read again, and their elements and the row's tail put in order.  The K-th best of
@@ -669,8 +669,9 @@ int64_t most_parts(int32_t top) {
 // unit at once.  Items that are up to half more than fit would leave most of the card
 // idle behind the first: two to a team then, where that deals the blocks evenly and an
 // item is long (2,048 rows of 131,072: 102 us, then 95; 8,192 of 32,768 with 5
-// alternatives, a wave each: 140, then 130; but 2,040 of 40,000, five tiles long, 51,
-// then 55, and 2,300 of 50,257, four and a half blocks a unit, 42, then 48).
+// alternatives, a wave each: 140, then 132; but 2,040 of 40,000, five tiles long, 51,
+// then 55, and 2,300 of 50,257, four and a half blocks a unit, 42, then 48).  Three turns
+// and two and a half were not measured and are dealt as they come.
 unsigned blocks_in_turns(int64_t work, int per_block, int64_t vecs) {
     const int64_t fit = 6 * 256 * per_block, two = cdiv(work, 2 * per_block);
     const bool even = cdiv(two, 256) * 256 - two <= two / 16;
