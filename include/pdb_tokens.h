@@ -21,7 +21,9 @@
  * call here does, so one word can watch many calls.
  *
  * Arithmetic: binary32 whatever the types, rounded once (to nearest even) where
- * a 16-bit result is stored; what passes its type's range is infinite.  The
+ * a 16-bit result is stored; what passes its type's range is infinite.  That
+ * holds of differences too: in a row whose finite logits lie more than binary32's
+ * largest value apart, the lower ones may count as -inf.  The
  * order of every sum follows from the call's sizes and, in pdb_embed_grad, from
  * all of its tokens, so a repeated call gives the same bits.
  */
