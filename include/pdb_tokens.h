@@ -2,8 +2,9 @@
  * pdb token operators: what a model over a vocabulary of tokens needs around
  * the layers between -- the rows of a table that tokens pick and that table's
  * gradient (or its SGD step in place), log probabilities of given tokens with
- * entropies and the best alternatives, their gradient, and distillation from a
- * teacher's top logits with its gradient.  C ABI, same conventions as pdb.h:
+ * entropies and the best alternatives, their gradient, distillation from a
+ * teacher's top logits with its gradient, and the verification of tokens that a
+ * small model drafted for a large one.  C ABI, same conventions as pdb.h:
  * caller-owned device pointers, work on the caller's stream, PDB_OK or a
  * negative pdb_status, nothing kept past the call.  Every entry point here is
  * asynchronous and can be recorded into a HIP graph (no host wait, no
@@ -139,6 +140,40 @@ int pdb_distill(const void *logits, int dtype, int64_t ldz, int64_t n, int64_t v
                 const int32_t *ids, const void *teacher, int teacher_dtype, int32_t k, float temp,
                 const float *weight, float *loss, void *dlogits, int64_t ldd, int32_t *status,
                 void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Largest k of pdb_draft_verify. */
+#define PDB_MAX_DRAFT 64
+
+/* Device workspace (bytes) of pdb_draft_verify.  Host-only arithmetic. */
+int pdb_draft_verify_workspace_bytes(int64_t b, int32_t k, int64_t v, size_t *bytes);
+
+/* Which of b sequences' drafted tokens stand, and the token that follows, so that the
+ * tokens are distributed as if each were drawn from the target (k = 0: one token is
+ * drawn for each sequence).  With p_j = softmax(target row j / temp), q_j =
+ * softmax(draft row j / temp), x_j the drafted tokens and u given numbers of [0, 1):
+ *   x_0, x_1, ... are accepted while  u_j q_j(x_j) < p_j(x_j);
+ *   at the first that is refused the next token is drawn from max(p_j - q_j, 0),
+ *   behind the last from p: the lowest index whose running sum of those weights
+ *   exceeds u_k times their sum.
+ * A token is drawn from p, too, where max(p_j - q_j, 0) is 0 throughout, and the last
+ * index of weight > 0 where no running sum exceeds (u = 1).  Probabilities and sums
+ * are binary64; logits more than 700 temp below their row's largest count as -inf.
+ * target: device, b (k + 1) x v, row stride ldt: sequence i's rows i (k + 1) + j.
+ * draft: device, b k x v, row stride ldq, of the same type: rows i k + j; or NULL for
+ * tokens proposed without a distribution (q_j = 1 at x_j).  tokens: device, b x k of
+ * `index` without gaps; a sequence's drafted tokens end at its first negative one
+ * (the logits behind are not used), and at one >= v, which sets *status as above.
+ * u: device, b x (k + 1) float without gaps.  out: device, b x (k + 1) int32 without
+ * gaps: the accepted tokens, the next one, then -1.  accepted: device, [b] int32.
+ * Rows of nothing but -inf, or with a NaN or +inf, have no distribution: as the
+ * target's they refuse, and the next token is -1; as the draft's, those of -inf have
+ * q = 0, the others refuse and leave p.  temp > 0 and finite.  0 <= k <=
+ * PDB_MAX_DRAFT, v > 0, b (k + 1) < 2^31.  ws: at least
+ * pdb_draft_verify_workspace_bytes(b, k, v). */
+int pdb_draft_verify(const void *target, int64_t ldt, const void *draft, int64_t ldq, int dtype,
+                     int64_t b, int32_t k, int64_t v, const void *tokens, int index,
+                     const float *u, float temp, int32_t *out, int32_t *accepted, int32_t *status,
+                     void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

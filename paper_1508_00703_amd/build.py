@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(os.path.dirname(HERE), "_build")
 LIB = os.path.join(HERE, "libpdb.so")
 SOURCES = ["radix.hip", "schedule.hip", "apply.hip", "batch.hip", "stale.hip", "dense.hip",
-           "embed.hip", "vocab.hip", "distill.hip", "abi.hip", "mb.hip"]
+           "embed.hip", "vocab.hip", "distill.hip", "verify.hip", "scan.hip", "clip.hip", "abi.hip",
+           "mb.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -1,0 +1,338 @@
+// The norm of many tensors together, and the clipped gradients or the clipped step by
+// it (gfx950, wave64).
+//
+// norm = |s| sqrt(sum g^2).  The tensors are cut into chunks; descriptions of up to
+// kMostTensors travel in a launch's arguments, so nothing is copied to the device.
+// Squares and sums are in binary64 (a square in binary32 passes its range from 1.8e19
+// on, and falls out of it below 1e-23); each block leaves one sum, and whoever needs
+// the norm adds the blocks' sums in the same order: no atomics.  Bound: the bytes.
+// Clipping cannot begin before the last gradient is read: a second pass, from the last
+// chunk to the first, so that it meets first what the cache still holds.
+#include <math.h>
+
+#include "pdb_vec.h"
+#include "../../include/pdb_layers.h"
+
+namespace pdbk {
+namespace {
+
+constexpr int kMostTensors = 64;  // of a launch: a lane each, 3.6 KB of arguments
+constexpr int kChunk = 8192;      // elements
+constexpr int kSums = 2048;       // blocks that the card holds, a sum of each
+
+struct Item {
+    const char *g;
+    char *o;
+    int64_t cols, ld, ldo;
+    int32_t rows;
+    uint32_t first;  // the tensor's first chunk in the launch
+    int16_t dt, odt;
+    int32_t rows_at_once;  // rows of a chunk; 1 where a row has several chunks
+};
+struct List {
+    Item item[kMostTensors];
+    int32_t count;
+    uint32_t chunks;
+};
+
+// A chunk: rows [row, row + rows) x columns [col, col + cols) of a tensor.
+struct Chunk {
+    int64_t row, col;
+    int32_t rows, cols;
+    int item;
+};
+__device__ __forceinline__ Chunk chunk_of(const List &list, uint32_t w) {
+    const int l = lane_id();
+    const bool at = l < list.count && list.item[l].first <= w;
+    const int i = __builtin_amdgcn_readfirstlane(__popcll(__ballot(at)) - 1);
+    const Item &t = list.item[i];
+    const uint32_t k = w - t.first;
+    if (t.rows == 1 || t.cols > kChunk) {
+        const uint32_t of_row = (uint32_t)((t.cols + kChunk - 1) / kChunk);
+        const uint32_t row = k / of_row;
+        const int64_t col = (int64_t)(k - row * of_row) * kChunk;
+        return {(int64_t)row, col, 1, (int32_t)min((int64_t)kChunk, t.cols - col), i};
+    }
+    const int64_t row = (int64_t)k * t.rows_at_once;
+    return {row, 0, (int32_t)min((int64_t)t.rows_at_once, t.rows - row), (int32_t)t.cols, i};
+}
+
+// Calls f(offset in g, offset in o, elements) for a thread's vectors of a chunk: whole
+// ones (elements = V), and what is left of rows.
+template <int V, typename F>
+__device__ __forceinline__ void for_vectors(const Item &t, const Chunk &c, F f) {
+    const int64_t g0 = c.row * t.ld + c.col, o0 = c.row * t.ldo + c.col;
+    const int whole = c.cols / V, rem = c.cols - whole * V;
+    if (c.rows == 1) {
+#pragma unroll 4
+        for (int v = threadIdx.x; v < whole; v += kBlock) f(g0 + v * V, o0 + v * V, V);
+        if ((int)threadIdx.x < rem)
+            f(g0 + whole * V + threadIdx.x, o0 + whole * V + threadIdx.x, 1);
+        return;
+    }
+    const uint32_t of_row = (uint32_t)(whole + (rem ? 1 : 0)), all = of_row * (uint32_t)c.rows;
+    for (uint32_t v = threadIdx.x; v < all; v += kBlock) {
+        const uint32_t r = v / of_row, q = (v - r * of_row) * V;
+        f(g0 + r * t.ld + q, o0 + r * t.ldo + q, min(V, c.cols - (int)q));
+    }
+}
+
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+// the sum over the block, the same in every thread
+__device__ __forceinline__ double block_sum_f64(double v) {
+    __shared__ double s[kBlock / kWave];
+    v = wave_sum_f64(v);
+    if (lane_id() == 0) s[wave_in_block()] = v;
+    __syncthreads();
+    v = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    return v;
+}
+static_assert(kBlock == 4 * kWave, "four waves");
+
+template <int DT>
+__device__ __forceinline__ double chunk_squares(const Item &t, const Chunk &c) {
+    constexpr int V = Elem<DT>::kVec;
+    double s[2] = {0.0, 0.0};
+    for_vectors<V>(t, c, [&](int64_t g, int64_t, int k) {
+        if (k == V) {
+            float x[V];
+            unpack<DT>(load16(elem_at<DT>(t.g, g)), x);
+#pragma unroll
+            for (int q = 0; q < V; ++q) s[q & 1] = fma((double)x[q], (double)x[q], s[q & 1]);
+        } else {
+            for (int q = 0; q < k; ++q) {
+                const double x = load1<DT>(t.g, g + q);
+                s[0] = fma(x, x, s[0]);
+            }
+        }
+    });
+    return s[0] + s[1];
+}
+
+// sums[block] (+)= the squares of the block's chunks
+__global__ __launch_bounds__(kBlock) void k_grad_squares(List list, double *sums, int add) {
+    double s = 0.0;
+    for (uint32_t w = blockIdx.x; w < list.chunks; w += gridDim.x) {
+        const Chunk c = chunk_of(list, w);
+        const Item &t = list.item[c.item];
+        if (t.dt == PDB_F32) s += chunk_squares<PDB_F32>(t, c);
+        if (t.dt == PDB_F16) s += chunk_squares<PDB_F16>(t, c);
+        if (t.dt == PDB_BF16) s += chunk_squares<PDB_BF16>(t, c);
+    }
+    s = block_sum_f64(s);
+    if (threadIdx.x == 0) sums[blockIdx.x] = add ? sums[blockIdx.x] + s : s;
+}
+
+__device__ __forceinline__ double norm_of(const double *sums, int count, double scale) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kSums / kBlock; ++i) {
+        const int at = i * kBlock + threadIdx.x;
+        s += at < count ? sums[at] : 0.0;
+    }
+    return fabs(scale) * sqrt(block_sum_f64(s));
+}
+
+__global__ __launch_bounds__(kBlock) void k_grad_norm(const double *sums, int count, double scale,
+                                                      float *norm) {
+    const double n = norm_of(sums, count, scale);
+    if (threadIdx.x == 0) *norm = (float)n;
+}
+
+template <int DT, int OT>
+__device__ __forceinline__ void chunk_step(const Item &t, const Chunk &c, float by, bool acc) {
+    // as many elements as one 16-byte load of the narrower type gives
+    constexpr int V = Elem<DT>::kVec > Elem<OT>::kVec ? Elem<DT>::kVec : Elem<OT>::kVec;
+    for_vectors<V>(t, c, [&](int64_t g, int64_t o, int k) {
+        if (k == V) {
+            float x[V], y[V];
+            load_elems<DT, V>(t.g, g, x);
+            if (acc) load_elems<OT, V>(t.o, o, y);
+#pragma unroll
+            for (int q = 0; q < V; ++q) y[q] = acc ? __builtin_fmaf(by, x[q], y[q]) : by * x[q];
+            store_elems<OT, V>(t.o, o, y);
+        } else {
+            for (int q = 0; q < k; ++q) {
+                const float x = load1<DT>(t.g, g + q);
+                const float y = acc ? __builtin_fmaf(by, x, load1<OT>(t.o, o + q)) : by * x;
+                store1<OT>(t.o, o + q, y);
+            }
+        }
+    });
+}
+
+__global__ __launch_bounds__(kBlock) void k_grad_clip(List list, const double *sums, int count,
+                                                      double scale, double most, double step,
+                                                      int acc, float *norm) {
+    const double n = norm_of(sums, count, scale);
+    const float nf = (float)n;
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = nf;
+    if (!(fabsf(nf) < __builtin_inff())) return;
+    const float by = (float)(step * (n > most ? most / n : 1.0) * scale);
+    for (uint32_t i = blockIdx.x; i < list.chunks; i += gridDim.x) {
+        const Chunk c = chunk_of(list, list.chunks - 1 - i);
+        const Item &t = list.item[c.item];
+        if (!acc && by == 1.0f && t.g == t.o) continue;
+        auto to = [&](auto dt) {
+            constexpr int DT = decltype(dt)::value;
+            if (t.odt == PDB_F32) chunk_step<DT, PDB_F32>(t, c, by, acc);
+            if (t.odt == PDB_F16) chunk_step<DT, PDB_F16>(t, c, by, acc);
+            if (t.odt == PDB_BF16) chunk_step<DT, PDB_BF16>(t, c, by, acc);
+        };
+        if (t.dt == PDB_F32) to(DtypeTag<PDB_F32>());
+        if (t.dt == PDB_F16) to(DtypeTag<PDB_F16>());
+        if (t.dt == PDB_BF16) to(DtypeTag<PDB_BF16>());
+    }
+}
+
+// ----------------------------------------------------------------------------
+// host side
+
+constexpr int64_t kMostElements = (int64_t)1 << 40;  // of a tensor: at most 2^28 chunks
+constexpr int64_t kMostAll = (int64_t)1 << 43;       // at most 2^31 chunks
+constexpr int64_t kMostChunks = (int64_t)1 << 30;    // a list is closed from here on
+constexpr int kMostLists = (1 << 20) / kMostTensors + 2;
+
+int check_tensor(const pdb_tensor &t) {
+    if (!is_dtype(t.dtype) || t.rows < 0 || t.cols < 0) return PDB_ERR_INVALID_ARG;
+    if (t.rows == 0 || t.cols == 0) return PDB_OK;
+    if (t.rows > INT32_MAX || t.cols >= kMostElements || t.rows >= kMostElements / t.cols ||
+        t.ld > kMostElements)
+        return PDB_ERR_UNSUPPORTED;
+    if (t.rows > 1 && t.ld < t.cols) return PDB_ERR_INVALID_ARG;
+    if (!t.data || !aligned_to(t.data, dtype_size(t.dtype))) return PDB_ERR_INVALID_ARG;
+    return PDB_OK;
+}
+
+int check_tensors(const pdb_tensor *grads, int64_t count, const pdb_tensor *outs) {
+    if (count < 0 || (count > 0 && !grads)) return PDB_ERR_INVALID_ARG;
+    if (count >= 1 << 20) return PDB_ERR_UNSUPPORTED;
+    int64_t all = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (int e = check_tensor(grads[i])) return e;
+        all += grads[i].rows * grads[i].cols;
+        if (all >= kMostAll) return PDB_ERR_UNSUPPORTED;
+        if (!outs) continue;
+        if (int e = check_tensor(outs[i])) return e;
+        if (outs[i].rows != grads[i].rows || outs[i].cols != grads[i].cols) return PDB_ERR_INVALID_ARG;
+        const bool some = grads[i].rows > 0 && grads[i].cols > 0;
+        if (some && outs[i].data == grads[i].data &&
+            (outs[i].dtype != grads[i].dtype || (outs[i].rows > 1 && outs[i].ld != grads[i].ld)))
+            return PDB_ERR_INVALID_ARG;
+    }
+    return PDB_OK;
+}
+
+// Adds tensors from `from` on to a list; the first that is not in it.
+int64_t fill_list(const pdb_tensor *grads, const pdb_tensor *outs, int64_t from, int64_t count,
+                  List *list) {
+    list->count = 0;
+    list->chunks = 0;
+    int64_t i = from;
+    for (; i < count && list->count < kMostTensors && list->chunks < kMostChunks; ++i) {
+        const pdb_tensor &g = grads[i];
+        if (g.rows == 0 || g.cols == 0) continue;
+        Item &t = list->item[list->count++];
+        t.g = static_cast<const char *>(g.data);
+        t.o = outs ? static_cast<char *>(outs[i].data) : nullptr;
+        t.dt = (int16_t)g.dtype;
+        t.odt = outs ? (int16_t)outs[i].dtype : 0;
+        t.rows = (int32_t)g.rows, t.cols = g.cols, t.ld = g.ld, t.ldo = outs ? outs[i].ld : 0;
+        if (t.rows > 1 && t.ld == t.cols && (!outs || t.ldo == t.cols)) {  // no gaps: one row
+            t.cols *= t.rows;
+            t.rows = 1;
+        }
+        t.rows_at_once = t.cols >= kChunk ? 1 : (int32_t)(kChunk / t.cols);
+        const int64_t chunks = t.rows == 1 || t.cols > kChunk ? t.rows * cdiv(t.cols, kChunk)
+                                                             : cdiv(t.rows, t.rows_at_once);
+        t.first = list->chunks;
+        list->chunks += (uint32_t)chunks;
+    }
+    return i;
+}
+
+// The sums of squares of all tensors; how many sums there are.
+int sum_squares(const pdb_tensor *grads, int64_t count, double *sums, int *blocks,
+                hipStream_t stream) {
+    List list;
+    uint32_t most = 1;
+    for (int64_t i = 0; i < count;) {
+        i = fill_list(grads, nullptr, i, count, &list);
+        most = std::max(most, list.chunks);
+    }
+    *blocks = (int)std::min<uint32_t>(most, kSums);
+    int64_t i = 0;
+    bool add = false;
+    do {
+        i = fill_list(grads, nullptr, i, count, &list);
+        if (list.count == 0 && add) break;
+        k_grad_squares<<<*blocks, kBlock, 0, stream>>>(list, sums, add);
+        PDB_LAUNCHED();
+        add = true;
+    } while (i < count);
+    return PDB_OK;
+}
+
+constexpr size_t kGradWs = kSums * sizeof(double);
+
+}  // namespace
+}  // namespace pdbk
+
+using namespace pdbk;
+
+extern "C" int pdb_grad_workspace_bytes(size_t *bytes) {
+    if (!bytes) return PDB_ERR_INVALID_ARG;
+    *bytes = kGradWs;
+    return PDB_OK;
+}
+
+extern "C" int pdb_grad_norm(const pdb_tensor *grads, int64_t count, float scale, float *norm,
+                             void *ws, size_t ws_bytes, hipStream_t stream) {
+    if (int e = check_tensors(grads, count, nullptr)) return e;
+    if (!isfinite(scale) || !norm || !aligned_to(norm, 4)) return PDB_ERR_INVALID_ARG;
+    if (!ws || !aligned_to(ws, 8) || ws_bytes < kGradWs) return PDB_ERR_WORKSPACE;
+    double *sums = static_cast<double *>(ws);
+    int blocks = 0;
+    if (int e = sum_squares(grads, count, sums, &blocks, stream)) return e;
+    k_grad_norm<<<1, kBlock, 0, stream>>>(sums, blocks, scale, norm);
+    PDB_LAUNCHED();
+    return PDB_OK;
+}
+
+extern "C" int pdb_grad_clip(const pdb_tensor *grads, int64_t count, float scale, float max_norm,
+                             float step, int accumulate, const pdb_tensor *outs, float *norm,
+                             void *ws, size_t ws_bytes, hipStream_t stream) {
+    if (count > 0 && !outs) return PDB_ERR_INVALID_ARG;
+    if (int e = check_tensors(grads, count, outs)) return e;
+    if (!isfinite(scale) || !isfinite(step) || !(max_norm >= 0.0f) || !norm || !aligned_to(norm, 4) ||
+        (accumulate != 0 && accumulate != 1))
+        return PDB_ERR_INVALID_ARG;
+    if (!ws || !aligned_to(ws, 8) || ws_bytes < kGradWs) return PDB_ERR_WORKSPACE;
+    double *sums = static_cast<double *>(ws);
+    int blocks = 0;
+    if (int e = sum_squares(grads, count, sums, &blocks, stream)) return e;
+    // the lists from the last to the first, as the chunks in them
+    List list;
+    bool first = true;
+    int64_t starts[kMostLists];
+    int64_t lists = 0;
+    for (int64_t i = 0; i < count; ++lists) {
+        starts[lists] = i;
+        i = fill_list(grads, outs, i, count, &list);
+    }
+    do {
+        const int64_t from = lists > 0 ? starts[--lists] : 0;
+        fill_list(grads, outs, from, count, &list);
+        const unsigned grid = std::max(std::min<uint32_t>(list.chunks, kSums), 1u);
+        k_grad_clip<<<grid, kBlock, 0, stream>>>(list, sums, blocks, scale, max_norm, step, accumulate,
+                                                first ? norm : nullptr);
+        PDB_LAUNCHED();
+        first = false;
+    } while (lists > 0);
+    return PDB_OK;
+}

@@ -7,6 +7,7 @@ there is no fallback path.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -32,7 +33,8 @@ PDB_EPOCH_AUTO, PDB_EPOCH_LEVELS, PDB_EPOCH_SYNCFREE = 0, 1, 2
 PDB_STALE_AUTO, PDB_STALE_SYNCFREE, PDB_STALE_WINDOWED = 0, 1, 2
 PDB_F32, PDB_F16, PDB_BF16 = 0, 1, 2
 PDB_I32, PDB_I64 = 0, 1
-PDB_MAX_TOP, PDB_MAX_TEACHER = 128, 1024
+PDB_MAX_TOP, PDB_MAX_TEACHER, PDB_MAX_DRAFT = 128, 1024, 64
+PDB_SCAN_MARK = 64
 
 # every symbol declared in include/*.h
 EXPORTS = (
@@ -49,6 +51,10 @@ EXPORTS = (
     "pdb_embed_lookup", "pdb_embed_grad_workspace_bytes", "pdb_embed_grad",
     "pdb_token_logprobs_workspace_bytes", "pdb_token_logprobs", "pdb_token_logprobs_grad",
     "pdb_distill_workspace_bytes", "pdb_distill",
+    "pdb_draft_verify_workspace_bytes", "pdb_draft_verify",
+    # include/pdb_layers.h
+    "pdb_gated_scan_workspace_bytes", "pdb_gated_scan", "pdb_gated_scan_grad",
+    "pdb_grad_workspace_bytes", "pdb_grad_norm", "pdb_grad_clip",
 )
 
 
@@ -161,6 +167,16 @@ def load() -> ctypes.CDLL:
     lib.pdb_distill_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
     lib.pdb_distill.argtypes = [P, i32, i64, i64, i64, P, P, i32, i32, f32, P, P, P, i64, P, P, sz,
                                 P]
+    lib.pdb_draft_verify_workspace_bytes.argtypes = [i64, i32, i64, ctypes.POINTER(sz)]
+    lib.pdb_draft_verify.argtypes = [P, i64, P, i64, i32, i64, i32, i64, P, i32, P, f32, P, P, P, P,
+                                     sz, P]
+    lib.pdb_gated_scan_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.pdb_gated_scan.argtypes = [P, i64, P, i64, i32, i64, i64, P, i64, P, P, i64, P, P, P, P, sz, P]
+    lib.pdb_gated_scan_grad.argtypes = [P, i64, P, i64, P, i64, i32, i64, i64, P, i64, P, P, P, P,
+                                        i64, P, i64, P, P, P, sz, P]
+    lib.pdb_grad_workspace_bytes.argtypes = [ctypes.POINTER(sz)]
+    lib.pdb_grad_norm.argtypes = [P, i64, f32, P, P, sz, P]
+    lib.pdb_grad_clip.argtypes = [P, i64, f32, f32, f32, i32, P, P, P, sz, P]
     for name in EXPORTS:
         if name not in ("pdb_strerror",):
             getattr(lib, name).restype = ctypes.c_int
@@ -662,6 +678,8 @@ def _on_own_device(call):
     @functools.wraps(call)
     def run(*args, **kw):
         first = args[0] if args else kw.get(name)
+        if isinstance(first, (list, tuple)):
+            first = first[0] if first else None
         if first is not None and first.is_cuda and first.get_device() != torch._C._cuda_getDevice():
             with torch.cuda.device(first.device):
                 return call(*args, **kw)
@@ -836,3 +854,246 @@ def pdb_distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, 
                               _status(status, dev), wp, size, _raw_stream(stream, dev)),
            "pdb_distill")
     return loss, out
+
+
+class DraftVerify:
+    """Output of pdb_draft_verify: tokens [b, k + 1] (int32: the accepted ones, the
+    next, then -1) and accepted [b] (int32)."""
+
+    __slots__ = ("tokens", "accepted")
+
+    def __init__(self, tokens, accepted):
+        self.tokens, self.accepted = tokens, accepted
+
+
+@functools.lru_cache(maxsize=256)
+def pdb_draft_verify_workspace_bytes(b: int, k: int, v: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().pdb_draft_verify_workspace_bytes(b, k, v, ctypes.byref(out)),
+           "pdb_draft_verify_workspace_bytes")
+    return out.value
+
+
+@_on_own_device
+def pdb_draft_verify(target: torch.Tensor, u: torch.Tensor, tokens=None, draft=None,
+                     temp: float = 1.0, ws=None, status=None, stream=None) -> DraftVerify:
+    """How many of the drafted tokens [b, k] stand against the target's logits
+    (b (k + 1) rows) and which token follows, from numbers u [b, k + 1] of [0, 1).
+    draft: the logits that the tokens were drawn from (b k rows), None where they
+    have none; both under softmax(logits / temp).  tokens None: one token is drawn
+    from each row of target."""
+    tp, tdt, ldt = _matrix(target, "target")
+    dev = target.get_device()
+    rows, v = target.shape
+    if tokens is not None and tokens.dim() != 2:
+        raise ValueError("tokens must be a matrix")
+    b, k = (rows, 0) if tokens is None else tokens.shape
+    if rows != b * (k + 1):
+        raise ValueError("target must have %d rows" % (b * (k + 1)))
+    kp, ix = _tokens(tokens, b * k, dev)
+    qp, ldq = None, 0
+    if draft is not None:
+        if draft.dtype != target.dtype or tuple(draft.shape) != (b * k, v):
+            raise ValueError("draft must have target's type and be %d x %d" % (b * k, v))
+        qp, _, ldq = _matrix(draft, "draft", dev)
+    wp, size, ws = _space(ws, pdb_draft_verify_workspace_bytes(b, k, v), target, stream)
+    out = _empty(target, (b, k + 1), torch.int32, stream)
+    accepted = _empty(target, b, torch.int32, stream)
+    _check(load().pdb_draft_verify(tp, ldt, qp, ldq, tdt, b, k, v, kp, ix,
+                                   _vector(u, "u", b * (k + 1), dev), temp, out.data_ptr(),
+                                   accepted.data_ptr(), _status(status, dev), wp, size,
+                                   _raw_stream(stream, dev)), "pdb_draft_verify")
+    return DraftVerify(out, accepted)
+
+
+# ---------------------------------------------------------------------------
+# layer operators (include/pdb_layers.h); the conventions of the token operators
+
+class GatedScan:
+    """Output of pdb_gated_scan: y as x, state [b, d] (float32, after every
+    sequence), marks (for the gradient; None if they were not asked for)."""
+
+    __slots__ = ("y", "state", "marks")
+
+    def __init__(self, y, state, marks):
+        self.y, self.state, self.marks = y, state, marks
+
+
+class GatedScanGrad:
+    """Output of pdb_gated_scan_grad: dx and dgate as x, dh0 [b, d] (None without
+    h0)."""
+
+    __slots__ = ("dx", "dgate", "dh0")
+
+    def __init__(self, dx, dgate, dh0):
+        self.dx, self.dgate, self.dh0 = dx, dgate, dh0
+
+
+@functools.lru_cache(maxsize=256)
+def pdb_gated_scan_workspace_bytes(n: int, d: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().pdb_gated_scan_workspace_bytes(n, d, ctypes.byref(out)),
+           "pdb_gated_scan_workspace_bytes")
+    return out.value
+
+
+def _sequences(x, starts, batch, dev):
+    """(address of the offsets or None, sequences) of the rows of x."""
+    b = batch
+    if starts is not None:
+        if starts.dim() != 1 or starts.numel() < 1 or batch not in (None, starts.numel() - 1):
+            raise ValueError("starts must be a vector of one more than the sequences")
+        return _vector(starts, "starts", starts.numel(), dev, torch.int32), starts.numel() - 1
+    if x.dim() == 3:
+        if batch not in (None, x.shape[0]):
+            raise ValueError("batch must be x's first size")
+        b = x.shape[0]
+    return None, 1 if b is None else b
+
+
+def _rows(t, name, x, dev):
+    """(address, row stride) of a tensor of x's type and shape, as a matrix of rows."""
+    if t.dtype != x.dtype or t.shape != x.shape:
+        raise ValueError("%s must have x's type and shape" % name)
+    if t.dim() == 3:
+        t = t.view(-1, t.shape[2])
+    p, _, ld = _matrix(t, name, dev)
+    return p, ld
+
+
+def _state(t, name, b, d, dev):
+    if t is not None and tuple(t.shape) != (b, d):
+        raise ValueError("%s must be %d x %d" % (name, b, d))
+    return _vector(t, name, b * d, dev)
+
+
+@_on_own_device
+def pdb_gated_scan(x: torch.Tensor, gate: torch.Tensor, starts=None, batch=None, h0=None,
+                   state=None, marks: bool = False, out=None, ws=None, status=None,
+                   stream=None) -> GatedScan:
+    """h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(gate), channel by channel
+    along the rows of each sequence.  x: n x d, whose sequences starts [b + 1]
+    (int32) begins and ends, or `batch` ones of equal length (1); or [b, t, d].  h0
+    [b, d]: first states, None for zeros.  state: where the last ones go (None: a
+    new tensor; h0 itself may be given).  marks: also what the gradient needs."""
+    m = x.view(-1, x.shape[2]) if x.dim() == 3 else x
+    xp, dt, ldx = _matrix(m, "x")
+    dev = x.get_device()
+    n, d = m.shape
+    gp, ldg = _rows(gate, "gate", x, dev)
+    sp, b = _sequences(x, starts, batch, dev)
+    hp = _state(h0, "h0", b, d, dev)
+    f = torch.float32
+    if out is None:
+        out = _empty(x, x.shape, x.dtype, stream)
+    yp, ldy = _rows(out, "out", x, dev)
+    if state is None:
+        state = _empty(x, (b, d), f, stream)
+    mk = _empty(x, (-(-n // PDB_SCAN_MARK), d), f, stream) if marks else None
+    wp, size, ws = _space(ws, pdb_gated_scan_workspace_bytes(n, d), x, stream)
+    _check(load().pdb_gated_scan(xp, ldx, gp, ldg, dt, n, d, sp, b, hp, yp, ldy,
+                                 _state(state, "state", b, d, dev),
+                                 mk.data_ptr() if marks else None, _status(status, dev), wp, size,
+                                 _raw_stream(stream, dev)), "pdb_gated_scan")
+    return GatedScan(out, state, mk)
+
+
+@_on_own_device
+def pdb_gated_scan_grad(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, marks: torch.Tensor,
+                        starts=None, batch=None, h0=None, d_state=None, ws=None, status=None,
+                        stream=None) -> GatedScanGrad:
+    """The gradients by x, gate and h0 from those by y (dy) and by the last states
+    (d_state [b, d], None for zeros); x, gate, starts, batch and h0 as pdb_gated_scan
+    had them, and the marks that it gave."""
+    m = x.view(-1, x.shape[2]) if x.dim() == 3 else x
+    xp, dt, ldx = _matrix(m, "x")
+    dev = x.get_device()
+    n, d = m.shape
+    gp, ldg = _rows(gate, "gate", x, dev)
+    yp, ldy = _rows(dy, "dy", x, dev)
+    sp, b = _sequences(x, starts, batch, dev)
+    hp = _state(h0, "h0", b, d, dev)
+    dx, dgate = _empty(x, x.shape, x.dtype, stream), _empty(x, x.shape, x.dtype, stream)
+    dh0 = None if h0 is None else _empty(x, (b, d), torch.float32, stream)
+    wp, size, ws = _space(ws, pdb_gated_scan_workspace_bytes(n, d), x, stream)
+    _check(load().pdb_gated_scan_grad(
+        yp, ldy, xp, ldx, gp, ldg, dt, n, d, sp, b, hp,
+        _state(marks, "marks", -(-n // PDB_SCAN_MARK), d, dev),
+        _state(d_state, "d_state", b, d, dev), dx.data_ptr(), d, dgate.data_ptr(), d,
+        None if dh0 is None else dh0.data_ptr(), _status(status, dev), wp, size,
+        _raw_stream(stream, dev)), "pdb_gated_scan_grad")
+    return GatedScanGrad(dx, dgate, dh0)
+
+
+@functools.lru_cache(maxsize=None)
+def pdb_grad_workspace_bytes() -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().pdb_grad_workspace_bytes(ctypes.byref(out)), "pdb_grad_workspace_bytes")
+    return out.value
+
+
+def _tensors(ts, name, device, flat):
+    """Array of pdb_tensor of the tensors, as one row each where `flat`."""
+    n = len(ts)
+    try:
+        kind = [_DTYPES[t.dtype] for t in ts]
+    except KeyError:
+        raise TypeError("%s must be float32, float16 or bfloat16" % name) from None
+    if set(map(torch.Tensor.get_device, ts)) - {device} or device < 0:
+        raise ValueError("%s must be on one device" % name)
+    a = array.array("q", bytes(40 * n))
+    a[0::5] = array.array("q", map(torch.Tensor.data_ptr, ts))
+    a[4::5] = array.array("q", kind)
+    if flat:
+        size = array.array("q", map(torch.Tensor.numel, ts))
+        a[1::5], a[2::5], a[3::5] = array.array("q", [1]) * n, size, size
+        return a
+    for i, t in enumerate(ts):
+        if t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1):
+            a[5 * i + 1], a[5 * i + 2] = t.shape
+            a[5 * i + 3] = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+        elif t.is_contiguous():
+            a[5 * i + 1], a[5 * i + 2], a[5 * i + 3] = 1, t.numel(), t.numel()
+        else:
+            raise ValueError("%s must be contiguous, or matrices with unit column stride" % name)
+    return a
+
+
+def _grads(grads):
+    if not grads:
+        raise ValueError("grads must hold at least one tensor")
+    return list(grads), grads[0].get_device()
+
+
+@_on_own_device
+def pdb_grad_norm(grads, scale: float = 1.0, ws=None, stream=None) -> torch.Tensor:
+    """|scale| times the norm of all the tensors together, a tensor of no dimension."""
+    grads, dev = _grads(grads)
+    g = _tensors(grads, "grads", dev, all(map(torch.Tensor.is_contiguous, grads)))
+    norm = _empty(grads[0], (), torch.float32, stream)
+    wp, size, ws = _space(ws, pdb_grad_workspace_bytes(), grads[0], stream)
+    _check(load().pdb_grad_norm(g.buffer_info()[0], len(grads), scale, norm.data_ptr(), wp, size,
+                                _raw_stream(stream, dev)), "pdb_grad_norm")
+    return norm
+
+
+@_on_own_device
+def pdb_grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, step: float = 1.0,
+                  accumulate: bool = False, ws=None, stream=None) -> torch.Tensor:
+    """step * scale * min(1, max_norm / norm) times the gradients, written to the
+    tensors out (None: in place) or, with accumulate, added to them (the parameters
+    and step = -lr: the clipped step); the norm, as pdb_grad_norm gives it.  Nothing is
+    written where that is not finite."""
+    grads, dev = _grads(grads)
+    out = grads if out is None else list(out)
+    if len(out) != len(grads) or any(a.shape != b.shape for a, b in zip(grads, out)):
+        raise ValueError("out must hold a tensor of the same shape for every gradient")
+    flat = all(map(torch.Tensor.is_contiguous, grads)) and all(map(torch.Tensor.is_contiguous, out))
+    g = _tensors(grads, "grads", dev, flat)
+    o = _tensors(out, "out", dev, flat)
+    norm = _empty(grads[0], (), torch.float32, stream)
+    wp, size, ws = _space(ws, pdb_grad_workspace_bytes(), grads[0], stream)
+    _check(load().pdb_grad_clip(g.buffer_info()[0], len(grads), scale, max_norm, step,
+                                1 if accumulate else 0, o.buffer_info()[0], norm.data_ptr(), wp, size,
+                                _raw_stream(stream, dev)), "pdb_grad_clip")
+    return norm
