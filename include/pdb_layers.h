@@ -39,13 +39,16 @@ int pdb_gated_scan_workspace_bytes(int64_t n, int64_t d, size_t *bytes);
  * nothing outside the outputs.
  * h0: device, b x d float without gaps, or NULL.  state: device, b x d float
  * without gaps, or NULL: h after every sequence's last row (its row of h0, or
- * zeros, where the sequence is empty); with n = b and no starts it may be h0 itself.  marks: device,
+ * zeros, where the sequence is empty); it may be h0 itself.  marks: device,
  * ceil(n / PDB_SCAN_MARK) x d float without gaps, or NULL: row i is the h that
  * enters row i * PDB_SCAN_MARK, for pdb_gated_scan_grad (unspecified where that
  * row is of no sequence).
  * A value that is not finite makes its channel not finite from its row to its
  * sequence's end, and reaches no other sequence.
- * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d). */
+ * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8,
+ * for this call alone until it has run (tiles of rows pass their states through it; a
+ * wait of 2 s there, which only a workspace that something else writes brings about,
+ * ends with NaN and *status = PDB_ERR_DEVICE). */
 int pdb_gated_scan(const void *x, int64_t ldx, const void *gate, int64_t ldg, int dtype, int64_t n,
                    int64_t d, const int32_t *starts, int64_t b, const float *h0, void *y,
                    int64_t ldy, float *state, float *marks, int32_t *status, void *ws,

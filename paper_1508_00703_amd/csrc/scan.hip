@@ -4,11 +4,15 @@
 // A row acts on the state as the map h -> a h + c, and maps compose: (a1, c1) then
 // (a2, c2) is (a2 a1, a2 c1 + c2).  The rows are cut into tiles of kTileRows, whatever
 // sequences they hold, and the channels into strips of 128 bytes of a row: a block has
-// a tile of a strip in registers, kRows rows of a vector of channels to a thread.  The
-// threads' maps are joined through LDS, the tiles' through the workspace.  A row that
-// begins a sequence takes its first state in place of what enters: its map is "cut",
-// a = -0 (gates are never negative, so products and selects keep the mark), and
-// nothing of another sequence passes it, not even a NaN.
+// a tile of a strip in registers, kRows rows of a vector of channels to a thread, and
+// reads it once.  The threads' maps are joined through LDS, the tiles' through the
+// workspace while the blocks run: each publishes its map, waits for the state behind
+// the tile kReach before and applies the maps between, in order (so the sums do not
+// depend on who was first), and publishes the state behind its own.  Tiles are dealt
+// by a counter, so a block waits only for blocks that have begun.  A row that begins a
+// sequence takes its first state in place of what enters: its map is "cut", a = -0
+// (gates are never negative, so products and selects keep the mark), and nothing of
+// another sequence passes it, not even a NaN.
 #include "pdb_vec.h"
 #include "pdb_softmax.h"
 #include "../../include/pdb_layers.h"
@@ -65,8 +69,10 @@ struct Scan {
     const float *marks_in;
     int32_t *status;
     int32_t tiles, strips;
-    Map *total;    // [tiles][strips][slots]: the tiles' maps
-    float *enter;  // the same: what enters the tiles
+    // in the order of the chain (the backward's from the last tile on); NULL of one tile
+    unsigned long long *total;  // [tiles][strips][slots]: the tiles' maps
+    uint32_t *leave;            // the same: the states behind them
+    uint32_t *ticket;  // [0]: tiles dealt; [1]: 0 once a wait has lasted too long
 };
 
 // The sequences that begin and end with the rows of a tile, -1 elsewhere.
@@ -95,7 +101,7 @@ __device__ __forceinline__ int starts_below(const int32_t *starts, int64_t count
 // (the last tile: or behind) get their states, those of `from`.
 template <int V, bool WIDE>
 __device__ __forceinline__ bool find_edges(const Scan &p, int64_t r0, bool last_tile, int64_t c0,
-                                           bool act, const float *from, Edges &e, int64_t &lo,
+                                           int own, bool act, const float *from, Edges &e, int64_t &lo,
                                            int64_t &hi) {
     int any = 0;
     const int t = threadIdx.x;
@@ -148,7 +154,7 @@ __device__ __forceinline__ bool find_edges(const Scan &p, int64_t r0, bool last_
                 const int64_t a0 = starts[i], a1 = starts[i + 1];
                 if (a1 > a0 || !(a0 < r1 || last_tile)) continue;
                 if (act && threadIdx.x < kStripLanes)
-                    for (int q = 0; q < V; ++q)
+                    for (int q = own; q < V; ++q)
                         if (WIDE || c0 + q < p.d)
                             p.state[i * p.d + c0 + q] = from ? from[i * p.d + c0 + q] : 0.0f;
             }
@@ -182,16 +188,17 @@ __device__ __forceinline__ u32x4 load_vec(const void *m, int64_t ld, int64_t row
         return pack<DT>(x);
     }
 }
+// Only from element `own` on: a row's last vector may share channels with the one before.
 template <int DT, bool WIDE>
 __device__ __forceinline__ void store_vec(void *m, int64_t ld, int64_t row, int64_t c0, int64_t d,
-                                          const float *x) {
+                                          int own, const float *x) {
     char *at = elem_at<DT>(m, row * ld + c0);
-    if constexpr (WIDE) {
+    if (WIDE && own == 0) {
         store16(at, pack<DT>(x));
     } else {
 #pragma unroll
         for (int q = 0; q < Elem<DT>::kVec; ++q)
-            if (q < d) store1<DT>(at, q, x[q]);
+            if (q >= own && (WIDE || q < d)) store1<DT>(at, q, x[q]);
     }
 }
 // V floats of row i of a b x d (or marks) array without gaps, zeros of NULL
@@ -201,10 +208,11 @@ __device__ __forceinline__ void load_row(const float *m, int64_t i, int64_t c0, 
     for (int q = 0; q < V; ++q) x[q] = m && (WIDE || q < d) ? m[i * d + c0 + q] : 0.0f;
 }
 template <int V, bool WIDE>
-__device__ __forceinline__ void store_row(float *m, int64_t i, int64_t c0, int64_t d, const float *x) {
+__device__ __forceinline__ void store_row(float *m, int64_t i, int64_t c0, int64_t d, int own,
+                                          const float *x) {
 #pragma unroll
     for (int q = 0; q < V; ++q)
-        if (WIDE || q < d) m[i * d + c0 + q] = x[q];
+        if (q >= own && (WIDE || q < d)) m[i * d + c0 + q] = x[q];
 }
 
 // What a block shares: the threads' maps, then what enters each thread's rows.
@@ -258,37 +266,131 @@ __device__ __forceinline__ void get_enter(const Shared<V> &s, int rl, int cl, fl
 template <int DT, bool WIDE>
 struct Place {
     static constexpr int V = Elem<DT>::kVec;
-    int tile, strip, rl, cl;
+    int turn, tile, strip, rl, cl, own;  // turn: the tile's place in the chain
     int64_t r0, row, c0;
     bool act;
-    __device__ __forceinline__ Place(const Scan &p, int64_t w) {
-        tile = (int)((uint32_t)w / (uint32_t)p.strips);
-        strip = (int)((uint32_t)w - (uint32_t)tile * (uint32_t)p.strips);
+    __device__ __forceinline__ Place(const Scan &p, uint32_t w, bool back) {
+        turn = (int)(w / (uint32_t)p.strips);
+        strip = (int)(w - (uint32_t)turn * (uint32_t)p.strips);
+        tile = back ? p.tiles - 1 - turn : turn;
         rl = threadIdx.x / kStripLanes;
         cl = threadIdx.x % kStripLanes;
         r0 = (int64_t)tile * kTileRows;
         row = r0 + rl * kRows;
-        // a strip's last vector ends with the row: it may share channels with the one
-        // before, which then stores the same values
+        // the last vector ends with the row: it may share channels with the one before,
+        // which has them (the states may be written over h0)
         const int64_t c = ((int64_t)strip * kStripLanes + cl) * V;
         act = c < p.d;
         c0 = WIDE ? min(c, p.d - V) : c;
-    }
-    __device__ __forceinline__ int64_t slot(const Scan &p) const {
-        return ((int64_t)tile * p.strips + strip) * (kStripLanes * V);
+        own = (int)(c - c0);
     }
 };
 
-// TOTAL: only the tiles' maps.
-template <int DT, bool WIDE, bool TOTAL>
+// The block's place in the chain's order.
+__device__ __forceinline__ uint32_t next_tile(const Scan &p) {
+    if (!p.ticket) return blockIdx.x;
+    __shared__ uint32_t w;
+    if (threadIdx.x == 0)
+        w = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return w;
+}
+
+constexpr int kReach = 16;
+constexpr int64_t kPatience = 200000000;  // ticks of the 100 MHz clock: 2 s
+constexpr int64_t kUneasy = 100000;       // 1 ms
+
+template <typename T>
+__device__ __forceinline__ T peek(const T *at) {
+    return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ void post(T *at, T word) {
+    __hip_atomic_store(at, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// The words of the chain carry their own readiness: all ones is "not yet" (a NaN that
+// no arithmetic here gives; one that comes from outside is replaced by another).
+__device__ __forceinline__ unsigned long long word_of(Map m) {
+    const unsigned long long w =
+        (unsigned long long)__float_as_uint(m.a) << 32 | __float_as_uint(m.c);
+    return w == ~0ull ? 0x7FC000007FC00000ull : w;
+}
+__device__ __forceinline__ Map map_of(unsigned long long w) {
+    return {__uint_as_float((uint32_t)(w >> 32)), __uint_as_float((uint32_t)w)};
+}
+__device__ __forceinline__ uint32_t word_of(float h) {
+    return __float_as_uint(h) == ~0u ? 0x7FC00000u : __float_as_uint(h);
+}
+
+// Whether a wait since t0 has lasted too long, here or in any other block: a chain whose
+// words were overwritten ends, in all its blocks.
+__device__ __forceinline__ bool give_up(const Scan &p, int64_t t0) {
+    const int64_t waited = now_ticks() - t0;
+    if (waited < kUneasy) return false;
+    if (peek(p.ticket + 1) == 0u) return true;
+    if (waited < kPatience) return false;
+    post(p.ticket + 1, 0u);
+    return true;
+}
+
+// What enters the tile at `turn` of strip `strip`, whose map is m: by the first wave, a
+// slot to a lane.  A wait that lasts kPatience ends with NaN and a status.
+template <int V>
+__device__ __forceinline__ float chain(const Scan &p, int turn, int strip, Map m) {
+    constexpr int kSlots = Shared<V>::kSlots;
+    if (!p.ticket) return 0.0f;
+    const int64_t slots = (int64_t)p.strips * kSlots;
+    const int64_t at = (int64_t)turn * slots + (int64_t)strip * kSlots + slot_of<V>();
+    const bool first_of_slot = lane_id() < kSlots, next = turn < p.tiles - 1;
+    if (next && first_of_slot) post(p.total + at, word_of(m));
+    unsigned long long w[kReach - 1];
+    uint32_t h = 0;
+    bool late = false;
+    const int64_t t0 = now_ticks();
+    if (turn >= kReach) {
+        while (true) {
+            h = peek(p.leave + (at - kReach * slots));
+            if (!__any(h == ~0u)) break;
+            if ((late = give_up(p, t0))) break;
+            __builtin_amdgcn_s_sleep(4);
+        }
+    }
+    const int maps = turn >= kReach ? kReach - 1 : turn;
+    while (!late) {
+        bool missing = false;
+#pragma unroll
+        for (int j = 0; j < kReach - 1; ++j) {
+            w[j] = 0;
+            if (j < maps) w[j] = peek(p.total + (at - (int64_t)(maps - j) * slots));
+        }
+#pragma unroll
+        for (int j = 0; j < kReach - 1; ++j) missing |= w[j] == ~0ull;
+        if (!__any(missing)) break;
+        late = give_up(p, t0);
+        __builtin_amdgcn_s_sleep(2);
+    }
+    float enter = __uint_as_float(h);
+    if (late) {
+        enter = kNan;  // seen by whoever uses the result
+        if (p.status) *p.status = PDB_ERR_DEVICE;
+    } else {
+#pragma unroll
+        for (int j = 0; j < kReach - 1; ++j)
+            if (j < maps) enter = apply(map_of(w[j]), enter);
+    }
+    if (turn + kReach < p.tiles && first_of_slot) post(p.leave + at, word_of(apply(m, enter)));
+    return enter;
+}
+
+template <int DT, bool WIDE>
 __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
     constexpr int V = Elem<DT>::kVec;
     __shared__ Shared<V> s;
-    const Place<DT, WIDE> at(p, blockIdx.x);
+    const Place<DT, WIDE> at(p, next_tile(p), false);
     int64_t lo, hi;
     const bool plain =
-        find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.c0, at.act && !TOTAL, p.h0, s.edges, lo, hi);
-    if constexpr (!TOTAL) check_starts(p);
+        find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.c0, at.own, at.act, p.h0, s.edges, lo, hi);
+    check_starts(p);
     float a[kRows][V], c[kRows][V];
     auto local = [&](auto is_plain) {
         constexpr bool kPlain = decltype(is_plain)::value;
@@ -315,8 +417,8 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
                 if (begin >= 0) {
                     if (at.act) load_row<V, WIDE>(p.h0, begin, at.c0, p.d, rc);
                     // now: when the states are written h0 may be gone
-                    if (!TOTAL && r == 0 && p.marks && row % PDB_SCAN_MARK == 0 && at.act)
-                        store_row<V, WIDE>(p.marks, row / PDB_SCAN_MARK, at.c0, p.d, rc);
+                    if (r == 0 && p.marks && row % PDB_SCAN_MARK == 0 && at.act)
+                        store_row<V, WIDE>(p.marks, row / PDB_SCAN_MARK, at.c0, p.d, at.own, rc);
 #pragma unroll
                     for (int q = 0; q < V; ++q) ra[q] = -0.0f;
                 }
@@ -338,17 +440,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
     put_part(s, at.rl, at.cl, a[kRows - 1], c[kRows - 1]);
     __syncthreads();
     if (wave_in_block() == 0) {
-        const int lane = lane_id();
-        if constexpr (TOTAL) {
-            const Map m = join_total<V, false>(s);
-            if (lane < Shared<V>::kSlots) p.total[at.slot(p) + lane] = m;
-        } else {
-            float h = 0.0f;
-            if (at.tile > 0) h = p.enter[at.slot(p) + slot_of<V>()];
-            join_enter<V, false>(s, h);
-        }
+        const Map m = join_total<V, false>(s);
+        join_enter<V, false>(s, chain<V>(p, at.turn, at.strip, m));
     }
-    if constexpr (TOTAL) return;
     __syncthreads();
     float h[V];
     get_enter(s, at.rl, at.cl, h);
@@ -356,7 +450,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
         constexpr bool kPlain = decltype(is_plain)::value;
         if (p.marks && at.row % PDB_SCAN_MARK == 0 && at.row < p.n &&
             (kPlain || s.edges.begin[at.rl * kRows] < 0))
-            store_row<V, WIDE>(p.marks, at.row / PDB_SCAN_MARK, at.c0, p.d, h);
+            store_row<V, WIDE>(p.marks, at.row / PDB_SCAN_MARK, at.c0, p.d, at.own, h);
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             const int64_t row = at.row + r;
@@ -366,10 +460,10 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
             for (int q = 0; q < V; ++q)
                 out[q] = kPlain ? __builtin_fmaf(a[r][q], h[q], c[r][q])
                                 : apply(Map{a[r][q], c[r][q]}, h[q]);
-            store_vec<DT, WIDE>(p.y, p.ldy, row, at.c0, p.d, out);
+            store_vec<DT, WIDE>(p.y, p.ldy, row, at.c0, p.d, at.own, out);
             if constexpr (!kPlain) {
                 const int end = s.edges.end[at.rl * kRows + r];
-                if (end >= 0 && p.state) store_row<V, WIDE>(p.state, end, at.c0, p.d, out);
+                if (end >= 0 && p.state) store_row<V, WIDE>(p.state, end, at.c0, p.d, at.own, out);
             }
         }
     };
@@ -383,15 +477,15 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
 // The backward pass of a tile.  Going back, a row acts on e (what the rows behind it
 // ask of the state before them) as e -> f (dy + e); a row that ends a sequence takes
 // d_state in place of e.  The states come from the mark that the tile begins with.
-template <int DT, bool WIDE, bool TOTAL>
+template <int DT, bool WIDE>
 __global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
     constexpr int V = Elem<DT>::kVec;
     __shared__ Shared<V> s;
-    const Place<DT, WIDE> at(p, blockIdx.x);
+    const Place<DT, WIDE> at(p, next_tile(p), true);
     int64_t lo, hi;
     const bool plain =
-        find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.c0, at.act && !TOTAL, p.d_state, s.edges, lo, hi);
-    if constexpr (!TOTAL) check_starts(p);
+        find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.c0, at.own, at.act, p.d_state, s.edges, lo, hi);
+    check_starts(p);
     float w[kRows][V], x[kRows][V];
     u32x4 ry[kRows];
     auto inside = [&](int64_t row) { return row >= lo && row < hi; };
@@ -404,7 +498,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
             if (at.act && (kPlain || at.row + r < p.n)) {
                 rg[r] = load_vec<DT, WIDE>(p.gate, p.ldg, at.row + r, at.c0, p.d);
                 ry[r] = load_vec<DT, WIDE>(p.dy, p.lddy, at.row + r, at.c0, p.d);
-                if (!TOTAL) rx[r] = load_vec<DT, WIDE>(p.x, p.ldx, at.row + r, at.c0, p.d);
+                rx[r] = load_vec<DT, WIDE>(p.x, p.ldx, at.row + r, at.c0, p.d);
             }
         }
 #pragma unroll
@@ -475,7 +569,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
             f(std::false_type());
     };
     both(load);
-    if constexpr (!TOTAL) {
+    {
         float h[V];
 #pragma unroll
         for (int q = 0; q < V; ++q) h[q] = 0.0f;
@@ -499,17 +593,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
     both(back);
     __syncthreads();
     if (wave_in_block() == 0) {
-        const int lane = lane_id();
-        if constexpr (TOTAL) {
-            const Map m = join_total<V, true>(s);
-            if (lane < Shared<V>::kSlots) p.total[at.slot(p) + lane] = m;
-        } else {
-            float e = 0.0f;
-            if (at.tile < p.tiles - 1) e = p.enter[at.slot(p) + slot_of<V>()];
-            join_enter<V, true>(s, e);
-        }
+        const Map m = join_total<V, true>(s);
+        join_enter<V, true>(s, chain<V>(p, at.turn, at.strip, m));
     }
-    if constexpr (TOTAL) return;
     __syncthreads();
     if (!at.act) return;
     float e[V];
@@ -531,27 +617,21 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
                 dg[q] = t * x[r][q] * (g.f * g.k);
                 e[q] = g.f * t;
             }
-            store_vec<DT, WIDE>(p.y, p.ldy, at.row + r, at.c0, p.d, dx);
-            store_vec<DT, WIDE>(p.dgate, p.lddg, at.row + r, at.c0, p.d, dg);
+            store_vec<DT, WIDE>(p.y, p.ldy, at.row + r, at.c0, p.d, at.own, dx);
+            store_vec<DT, WIDE>(p.dgate, p.lddg, at.row + r, at.c0, p.d, at.own, dg);
             if constexpr (!kPlain) {
                 const int begin = s.edges.begin[at.rl * kRows + r];
-                if (begin >= 0 && p.state) store_row<V, WIDE>(p.state, begin, at.c0, p.d, e);
+                if (begin >= 0 && p.state) store_row<V, WIDE>(p.state, begin, at.c0, p.d, at.own, e);
             }
         }
     });
 }
 
-// What enters every tile, from the tiles' maps: a slot to a thread.
-__global__ __launch_bounds__(kWave) void k_scan_enter(const Map *total, float *enter, int tiles,
-                                                      int64_t slots, int back) {
-    const int64_t slot = (int64_t)blockIdx.x * kWave + threadIdx.x;
-    if (slot >= slots) return;
-    float h = 0.0f;
-    for (int i = 0; i < tiles; ++i) {
-        const int64_t t = back ? tiles - 1 - i : i;
-        enter[t * slots + slot] = h;
-        h = apply(total[t * slots + slot], h);
-    }
+// A chain's words before it begins.
+__global__ __launch_bounds__(kBlock) void k_scan_clear(uint32_t *words, int64_t count) {
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < count;
+         i += (int64_t)gridDim.x * kBlock)
+        words[i] = i == 0 ? 0u : ~0u;
 }
 
 // Sequences of one row each: no state but the one that is given passes along.
@@ -566,30 +646,16 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(Scan p, int64_t vecs) {
     unpack<DT>(load_vec<DT, WIDE>(p.x, p.ldx, i, c0, p.d), x);
     unpack<DT>(load_vec<DT, WIDE>(p.gate, p.ldg, i, c0, p.d), g);
     load_row<V, WIDE>(p.h0, i, c0, p.d, h);
-    if (p.marks && i % PDB_SCAN_MARK == 0) {
-#pragma unroll
-        for (int q = 0; q < V; ++q)
-            if (c0 + q >= c && (WIDE || q < p.d)) p.marks[i / PDB_SCAN_MARK * p.d + c0 + q] = h[q];
-    }
+    const int own = (int)(c - c0);
+    if (p.marks && i % PDB_SCAN_MARK == 0)
+        store_row<V, WIDE>(p.marks, i / PDB_SCAN_MARK, c0, p.d, own, h);
 #pragma unroll
     for (int q = 0; q < V; ++q) {
         const Gate k = open_gate(small_gate(g[q]));
         h[q] = __builtin_fmaf(k.f, h[q], k.k * x[q]);
     }
-    // Where vectors overlap (c0 < c) and the state is h0 itself, the vector before may
-    // have written its channels already: each writes only its own.
-    if (c0 == c) {
-        store_vec<DT, WIDE>(p.y, p.ldy, i, c0, p.d, h);
-    } else {
-#pragma unroll
-        for (int q = 0; q < V; ++q)
-            if (c0 + q >= c) store1<DT>(p.y, i * p.ldy + c0 + q, h[q]);
-    }
-    if (p.state) {
-#pragma unroll
-        for (int q = 0; q < V; ++q)
-            if (c0 + q >= c && (WIDE || q < p.d)) p.state[i * p.d + c0 + q] = h[q];
-    }
+    store_vec<DT, WIDE>(p.y, p.ldy, i, c0, p.d, own, h);
+    if (p.state) store_row<V, WIDE>(p.state, i, c0, p.d, own, h);
 }
 
 // No rows at all: the states are the first ones, or zeros.
@@ -606,9 +672,10 @@ Cut cut_of(int64_t n, int64_t d, int dtype) {
     const int64_t v = 16 / dtype_size(dtype), strips = cdiv(std::max<int64_t>(d, 1), kStripLanes * v);
     return {std::max<int64_t>(cdiv(n, kTileRows), 1), strips, strips * kStripLanes * v};
 }
+// The chain's words: the counter (in a line of its own), the maps, the states.
+int64_t scan_words(const Cut &c) { return kAlign / 4 + c.tiles * c.slots * 3; }
 size_t scan_ws_bytes(int64_t n, int64_t d) {
-    const Cut c = cut_of(n, d, PDB_BF16);  // the widest strips
-    return (size_t)(align_up(c.tiles * c.slots * 8) + align_up(c.tiles * c.slots * 4));
+    return (size_t)align_up(scan_words(cut_of(n, d, PDB_BF16)) * 4);  // the widest strips
 }
 
 template <bool GRAD>
@@ -621,12 +688,15 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
         PDB_LAUNCHED();
         return PDB_OK;
     }
-    if (!ws || ws_bytes < scan_ws_bytes(p.n, p.d)) return PDB_ERR_WORKSPACE;
+    if (!ws || !aligned_to(ws, 8) || ws_bytes < scan_ws_bytes(p.n, p.d)) return PDB_ERR_WORKSPACE;
     if (cut.tiles * cut.strips > INT32_MAX) return PDB_ERR_UNSUPPORTED;
     p.tiles = (int32_t)cut.tiles;
     p.strips = (int32_t)cut.strips;
-    p.total = static_cast<Map *>(ws);
-    p.enter = reinterpret_cast<float *>(static_cast<char *>(ws) + align_up(cut.tiles * cut.slots * 8));
+    if (cut.tiles > 1) {
+        p.ticket = static_cast<uint32_t *>(ws);
+        p.total = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + kAlign);
+        p.leave = reinterpret_cast<uint32_t *>(p.total + cut.tiles * cut.slots);
+    }
     return with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         auto go = [&](auto wide) -> int {
@@ -639,18 +709,14 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
                 PDB_LAUNCHED();
                 return PDB_OK;
             }
-            if (cut.tiles > 1) {
-                if constexpr (GRAD)
-                    k_scan_grad<DT, W, true><<<grid, kBlock, 0, stream>>>(p);
-                else
-                    k_scan<DT, W, true><<<grid, kBlock, 0, stream>>>(p);
-                k_scan_enter<<<(unsigned)cdiv(cut.slots, kWave), kWave, 0, stream>>>(
-                    p.total, p.enter, p.tiles, cut.slots, GRAD);
+            if (p.ticket) {
+                const int64_t words = scan_words(cut);
+                k_scan_clear<<<grid_for(words, kBlock * 4, 2048), kBlock, 0, stream>>>(p.ticket, words);
             }
             if constexpr (GRAD)
-                k_scan_grad<DT, W, false><<<grid, kBlock, 0, stream>>>(p);
+                k_scan_grad<DT, W><<<grid, kBlock, 0, stream>>>(p);
             else
-                k_scan<DT, W, false><<<grid, kBlock, 0, stream>>>(p);
+                k_scan<DT, W><<<grid, kBlock, 0, stream>>>(p);
             PDB_LAUNCHED();
             return PDB_OK;
         };

@@ -159,6 +159,23 @@ def test_scan_shapes_and_states(gpu):
     torch.testing.assert_close(h, whole.state, rtol=1e-5, atol=1e-5)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,b", [(5000, 65, 7), (3000, 130, 2), (700, 9, 40), (2000, 5, 3)])
+def test_states_in_place(gpu, n, d, b, dtype):
+    """Text read in pieces: the last states written over the first ones."""
+    import torch
+
+    native = native_mod()
+    rng = np.random.default_rng(n)
+    x, _, g, _, starts, _, h0 = draw_scan(gpu, rng, n, d, b, "all", 0, 0, dtype)
+    h = torch.from_numpy(h0).to(gpu)
+    want = native.pdb_gated_scan(x, g, starts=starts, h0=h, marks=True)
+    for _ in range(5):
+        now = h.clone()
+        f = native.pdb_gated_scan(x, g, starts=starts, h0=now, state=now, marks=True)
+        assert torch.equal(f.y, want.y) and torch.equal(now, want.state) and torch.equal(f.marks, want.marks)
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 def test_values_that_are_not_finite_stay_in_their_sequence(gpu, bad):
     import torch
