@@ -2,17 +2,19 @@
 // backward pass (gfx950, wave64).
 //
 // A row acts on the state as the map h -> a h + c, and maps compose: (a1, c1) then
-// (a2, c2) is (a2 a1, a2 c1 + c2).  The rows are cut into tiles of kTileRows, whatever
-// sequences they hold, and the channels into strips of 128 bytes of a row: a block has
-// a tile of a strip in registers, kRows rows of a vector of channels to a thread, and
-// reads it once.  The threads' maps are joined through LDS, the tiles' through the
-// workspace while the blocks run: each publishes its map, waits for the state behind
-// the tile kReach before and applies the maps between, in order (so the sums do not
-// depend on who was first), and publishes the state behind its own.  Tiles are dealt
-// by a counter, so a block waits only for blocks that have begun.  A row that begins a
-// sequence takes its first state in place of what enters: its map is "cut", a = -0
-// (gates are never negative, so products and selects keep the mark), and nothing of
-// another sequence passes it, not even a NaN.
+// (a2, c2) is (a2 a1, a2 c1 + c2).  The rows are cut into tiles, whatever sequences they
+// hold, and the channels into strips of 128 bytes of a row: a block has a tile of a strip
+// in registers, some rows of a vector of channels to a thread, and reads it once.  The
+// threads' maps are joined through LDS, the tiles' through the workspace while the blocks
+// run: each publishes its map, waits for the state behind the tile kReach before and
+// applies the maps between, in order (so the sums do not depend on who was first), and
+// publishes the state behind its own.  Tiles are dealt by a counter, so a block waits
+// only for blocks that have begun.  A row that begins a sequence takes its first state in
+// place of what enters: its map is "cut", a = -0 (gates are never negative, so products
+// and selects keep the mark), and nothing of another sequence passes it, not even a NaN.
+//
+// The bound is the bytes; what stands before it is waiting: a tile's loads, the join, the
+// chain (about 1 us a hop over the card).  
 #include "pdb_vec.h"
 #include "pdb_softmax.h"
 #include "../../include/pdb_layers.h"
@@ -20,12 +22,19 @@
 namespace pdbk {
 namespace {
 
-constexpr int kStripLanes = 8;                         // lanes over 128 bytes of a row
-constexpr int kRowLanes = kBlock / kStripLanes;        // 32
-constexpr int kRows = 8;                               // rows of a thread
-constexpr int kTileRows = kRowLanes * kRows;           // 256
-static_assert(kTileRows % PDB_SCAN_MARK == 0 && PDB_SCAN_MARK % kRows == 0,
-              "a mark is at the first row of some thread");
+constexpr int kStripLanes = 8;                   // lanes over 128 bytes of a row
+constexpr int kRowLanes = kBlock / kStripLanes;  // 32
+
+// Rows of a thread: two numbers an element, in the backward four.
+template <int DT, bool BACK>
+struct Shape {
+    static constexpr int V = Elem<DT>::kVec;
+    static constexpr int kRows = BACK ? 4 : 8;
+    static constexpr int kTileRows = kRowLanes * kRows;
+    static constexpr int kSlots = kStripLanes * V;  // channels of a strip
+    static_assert(kTileRows % PDB_SCAN_MARK == 0 && PDB_SCAN_MARK % kRows == 0,
+                  "a mark is at the first row of some thread");
+};
 
 struct Map {
     float a, c;
@@ -39,19 +48,14 @@ __device__ __forceinline__ Map then(Map first, Map second) {
     return is_cut(second.a) ? second : Map{second.a * first.a, __builtin_fmaf(second.a, first.c, second.c)};
 }
 
-// A gate as the smaller of f and 1 - f, negative (also -0) where that is 1 - f: both
-// keep their relative accuracy, at either end.
-__device__ __forceinline__ float small_gate(float g) {
-    const float t = exp2_raw(-fabsf(g) * kLog2e);
-    const float s = t * __builtin_amdgcn_rcpf(1.0f + t);
-    return __uint_as_float(__float_as_uint(s) | (~__float_as_uint(g) & 0x80000000u));
-}
+// f = 1 / (1 + e^-g) and k = 1 - f, each with its own relative accuracy at either end.
 struct Gate {
-    float f, k;  // k = 1 - f
+    float f, k;
 };
-__device__ __forceinline__ Gate open_gate(float w) {
-    const float s = fabsf(w), l = 1.0f - s;
-    return (int)__float_as_uint(w) < 0 ? Gate{l, s} : Gate{s, l};
+__device__ __forceinline__ Gate gate_of(float g) {
+    const float t = exp2_raw(-fabsf(g) * kLog2e);
+    const float l = __builtin_amdgcn_rcpf(1.0f + t), s = t * l;
+    return g < 0.0f ? Gate{s, l} : Gate{l, s};
 }
 
 struct Scan {
@@ -72,12 +76,21 @@ struct Scan {
     // in the order of the chain (the backward's from the last tile on); NULL of one tile
     unsigned long long *total;  // [tiles][strips][slots]: the tiles' maps
     uint32_t *leave;            // the same: the states behind them
-    uint32_t *ticket;  // [0]: tiles dealt; [1]: 0 once a wait has lasted too long
+    uint32_t *ticket;           // [0]: tiles dealt; [1]: 0 once a wait has lasted too long
+    int32_t *first;             // [tiles]: what first_edge says of each
 };
 
-// The sequences that begin and end with the rows of a tile, -1 elsewhere.
+// ----------------------------------------------------------------------------
+// rows and sequences
+
+// A tile's rows of sequences, [lo, hi), and which sequences begin and end with its rows
+// (-1 elsewhere).
+template <int N>
 struct Edges {
-    int32_t begin[kTileRows], end[kTileRows];
+    int32_t begin[N], end[N];
+    int64_t lo, hi;
+    uint32_t dealt;  // the tile's place in the chain's order
+    int32_t first;
 };
 
 // How many of starts[0 .. b] lie below `row`: a search in 64 parts, the same in every
@@ -96,72 +109,94 @@ __device__ __forceinline__ int starts_below(const int32_t *starts, int64_t count
     return (int)lo;
 }
 
-// Fills `e` for the rows from r0 on; [lo, hi) are the rows of sequences.  True if the
-// tile has neither edges nor rows of no sequence.  Empty sequences at the tile's rows
-// (the last tile: or behind) get their states, those of `from`.
+// A strip's channels are in slots: channel q of the vector of lane cl in slot
+// q kStripLanes + cl, so that neighbouring lanes' are neighbours in LDS (vector by vector
+// the threads' maps met in the same banks: a third of the backward's time).
+__device__ __forceinline__ constexpr int slot_at(int q, int cl) { return q * kStripLanes + cl; }
+
+// The channel of a slot of a strip, -1 of none; `own`: -1 also where it is the vector's
+// before, with which the row's last one shares channels.
 template <int V, bool WIDE>
-__device__ __forceinline__ bool find_edges(const Scan &p, int64_t r0, bool last_tile, int64_t c0,
-                                           int own, bool act, const float *from, Edges &e, int64_t &lo,
-                                           int64_t &hi) {
-    int any = 0;
-    const int t = threadIdx.x;
-    e.begin[t] = e.end[t] = -1;
-    static_assert(kTileRows == kBlock, "a row to a thread");
+__device__ __forceinline__ int64_t channel_of(const Scan &p, int strip, int slot, bool own) {
+    const int64_t c = ((int64_t)strip * kStripLanes + slot % kStripLanes) * V;
+    const int64_t at = (WIDE ? min(c, p.d - V) : c) + slot / kStripLanes;
+    return c < p.d && at < p.d && !(own && at < c) ? at : -1;
+}
+
+// kPlain if the rows [r0, r1) neither begin nor end a sequence and all belong to one;
+// else the first of the offsets that lies at r0 or behind (0 without offsets).  By one
+// wave.
+constexpr int32_t kPlain = -1;
+__device__ __forceinline__ int32_t first_edge(const Scan &p, int64_t r0, int64_t r1, bool last_tile) {
     if (!p.starts) {
-        lo = 0;
-        hi = p.n;
-        const int64_t r = r0 + t;
-        if (r < p.n) {
-            const uint32_t s = (uint32_t)r / (uint32_t)p.len, o = (uint32_t)r - s * (uint32_t)p.len;
-            if (o == 0) e.begin[t] = (int)s;
-            if (o == (uint32_t)p.len - 1) e.end[t] = (int)s;
-            any = e.begin[t] >= 0 || e.end[t] >= 0;
-        } else {
-            any = 1;
-        }
-        return !__syncthreads_or(any);
+        const uint32_t o = (uint32_t)r0 % (uint32_t)max(p.len, 1);
+        return r1 <= p.n && o > 0 && o + (r1 - r0) < (uint32_t)p.len ? kPlain : 0;
     }
-    __syncthreads();
     const int32_t *starts = p.starts;
-    lo = std::max<int64_t>(starts[0], 0);
-    hi = std::min<int64_t>(starts[p.b], p.n);
-    if (r0 < lo || r0 + kTileRows > hi) any = 1;
-    const int64_t r1 = r0 + kTileRows;
-    const int64_t first = starts_below(starts, (int64_t)p.b + 1, r0 + (r0 == 0 ? INT32_MIN : 0));
-    // all threads take part in a turn, so that the empty sequences' states are written
-    // by whole rows of lanes
-    for (int64_t j0 = first;; j0 += kBlock) {
-        const int64_t j = j0 + t;
-        const bool have = j <= p.b;
-        const int64_t at = have ? starts[j] : INT64_MAX;
-        const int64_t next = j < p.b ? starts[j + 1] : INT64_MAX;
-        const int64_t before = have && j > 0 ? starts[j - 1] : INT64_MIN;
-        const bool mine = have && (at < r1 || last_tile);
-        if (have && at <= r1) {
-            if (j < p.b && at < next && at >= r0 && at < r1) {
-                e.begin[at - r0] = (int)j;
-                any = 1;
-            }
-            if (j > 0 && before < at && at > r0) {
-                e.end[at - 1 - r0] = (int)j - 1;
-                any = 1;
-            }
+    const int64_t lo = starts[0], hi = starts[p.b];
+    const int at = starts_below(starts, (int64_t)p.b + 1, r0 + (r0 == 0 ? INT32_MIN : 0));
+    const int64_t next = at <= p.b ? starts[at] : INT64_MAX;
+    // (a tile that ends with a sequence's last row has an edge: the offset is r1)
+    return r0 >= lo && r1 <= min(hi, p.n) && !last_tile && next > r1 ? kPlain : at;
+}
+
+// Fills `e` for the rows from r0 on, by one wave; first: what first_edge gave.  Empty
+// sequences at the tile's rows (the last tile: or behind) get their states, those of
+// `from`.
+template <int V, bool WIDE, int N>
+__device__ __forceinline__ void find_edges(const Scan &p, int64_t r0, bool last_tile, int strip,
+                                           const float *from, int32_t first, Edges<N> &e) {
+    const int l = lane_id();
+    for (int i = l; i < N; i += kWave) e.begin[i] = e.end[i] = -1;
+    Team<1>::sync();
+    int64_t lo = 0, hi = p.n;
+    const int64_t r1 = r0 + N;
+    if (!p.starts) {
+        for (int i = l; i < N; i += kWave) {
+            const int64_t r = r0 + i;
+            if (r >= p.n) break;
+            const uint32_t s = (uint32_t)r / (uint32_t)p.len, o = (uint32_t)r - s * (uint32_t)p.len;
+            if (o == 0) e.begin[i] = (int)s;
+            if (o == (uint32_t)p.len - 1) e.end[i] = (int)s;
         }
-        const bool none = mine && j < p.b && next <= at;
-        if (__syncthreads_or(none) && p.state) {
-            // rare: walk the turn's sequences, the empty ones' states by their channels
-            for (int64_t i = j0; i < std::min<int64_t>(j0 + kBlock, p.b); ++i) {
-                const int64_t a0 = starts[i], a1 = starts[i + 1];
-                if (a1 > a0 || !(a0 < r1 || last_tile)) continue;
-                if (act && threadIdx.x < kStripLanes)
-                    for (int q = own; q < V; ++q)
-                        if (WIDE || c0 + q < p.d)
-                            p.state[i * p.d + c0 + q] = from ? from[i * p.d + c0 + q] : 0.0f;
+    } else {
+        const int32_t *starts = p.starts;
+        lo = max((int64_t)starts[0], (int64_t)0);
+        hi = min((int64_t)starts[p.b], p.n);
+        for (int64_t j0 = first;; j0 += kWave) {
+            const int64_t j = j0 + l;
+            const bool have = j <= p.b;
+            const int64_t at = have ? starts[j] : INT64_MAX;
+            const int64_t next = j < p.b ? starts[j + 1] : INT64_MAX;
+            const int64_t before = have && j > 0 ? starts[j - 1] : INT64_MIN;
+            if (have && at <= r1) {
+                if (j < p.b && at < next && at >= r0 && at < r1) e.begin[at - r0] = (int)j;
+                if (j > 0 && before < at && at > r0) e.end[at - 1 - r0] = (int)j - 1;
             }
+            const bool none = have && j < p.b && next <= at && (at < r1 || last_tile);
+            for (unsigned long long m = p.state ? __ballot(none) : 0ull; m; m &= m - 1) {
+                const int64_t i = j0 + __ffsll(m) - 1;  // rare: a channel to a lane
+                const int64_t c = l < kStripLanes * V ? channel_of<V, WIDE>(p, strip, l, true) : -1;
+                if (c >= 0)
+                    p.state[i * p.d + c] = from ? from[i * p.d + c] : 0.0f;
+            }
+            if (!__any(have && at <= r1)) break;
         }
-        if (!__syncthreads_or(have && at <= r1)) break;
     }
-    return !__syncthreads_or(any);
+    if (l == 0) {
+        e.lo = lo;
+        e.hi = hi;
+    }
+}
+
+// Whether a wave's rows of a tile have no edges and are all of sequences.
+template <int N>
+__device__ __forceinline__ bool plain_wave(const Edges<N> &e, int64_t r0, int wave) {
+    constexpr int kOf = N / (kBlock / kWave);
+    static_assert(kOf <= kWave, "a row to a lane");
+    const int i = wave * kOf + lane_id() % kOf;
+    const bool edge = e.begin[i] >= 0 || e.end[i] >= 0 || r0 + i < e.lo || r0 + i >= e.hi;
+    return !__any(edge);
 }
 
 // Offsets that descend or leave 0 .. n, a share of them to a block.
@@ -215,67 +250,23 @@ __device__ __forceinline__ void store_row(float *m, int64_t i, int64_t c0, int64
         if (q >= own && (WIDE || q < d)) m[i * d + c0 + q] = x[q];
 }
 
-// What a block shares: the threads' maps, then what enters each thread's rows.
-template <int V>
-struct Shared {
-    static constexpr int kSlots = kStripLanes * V;
-    Map part[kRowLanes][kSlots];
-    float enter[kRowLanes][kSlots];
-    Edges edges;
-};
-
-// The slot of a lane of the first wave (strips of 32-bit channels: of two lanes).
-template <int V>
-__device__ __forceinline__ int slot_of() {
-    return lane_id() & (Shared<V>::kSlots - 1);
-}
-
-// Joins the threads' maps (in row order, or from the last row lane to the first) by the
-// first wave, a slot to a lane: total is the tile's map.
-template <int V, bool BACK>
-__device__ __forceinline__ Map join_total(const Shared<V> &s) {
-    const int slot = slot_of<V>();
-    Map m = s.part[BACK ? kRowLanes - 1 : 0][slot];
-#pragma unroll 8
-    for (int r = 1; r < kRowLanes; ++r) m = then(m, s.part[BACK ? kRowLanes - 1 - r : r][slot]);
-    return m;
-}
-template <int V, bool BACK>
-__device__ __forceinline__ void join_enter(Shared<V> &s, float h) {
-    const int slot = slot_of<V>();
-#pragma unroll 8
-    for (int i = 0; i < kRowLanes; ++i) {
-        const int r = BACK ? kRowLanes - 1 - i : i;
-        s.enter[r][slot] = h;
-        h = apply(s.part[r][slot], h);
-    }
-}
-
-template <int V>
-__device__ __forceinline__ void put_part(Shared<V> &s, int rl, int cl, const float *a, const float *c) {
-#pragma unroll
-    for (int q = 0; q < V; ++q) s.part[rl][cl * V + q] = Map{a[q], c[q]};
-}
-template <int V>
-__device__ __forceinline__ void get_enter(const Shared<V> &s, int rl, int cl, float *h) {
-#pragma unroll
-    for (int q = 0; q < V; ++q) h[q] = s.enter[rl][cl * V + q];
-}
+// ----------------------------------------------------------------------------
+// tiles
 
 // Where a block and a thread are.
-template <int DT, bool WIDE>
+template <int DT, bool WIDE, bool BACK>
 struct Place {
-    static constexpr int V = Elem<DT>::kVec;
+    static constexpr int V = Elem<DT>::kVec, kRows = Shape<DT, BACK>::kRows;
     int turn, tile, strip, rl, cl, own;  // turn: the tile's place in the chain
     int64_t r0, row, c0;
     bool act;
-    __device__ __forceinline__ Place(const Scan &p, uint32_t w, bool back) {
+    __device__ __forceinline__ Place(const Scan &p, uint32_t w) {
         turn = (int)(w / (uint32_t)p.strips);
         strip = (int)(w - (uint32_t)turn * (uint32_t)p.strips);
-        tile = back ? p.tiles - 1 - turn : turn;
+        tile = BACK ? p.tiles - 1 - turn : turn;
         rl = threadIdx.x / kStripLanes;
         cl = threadIdx.x % kStripLanes;
-        r0 = (int64_t)tile * kTileRows;
+        r0 = (int64_t)tile * Shape<DT, BACK>::kTileRows;
         row = r0 + rl * kRows;
         // the last vector ends with the row: it may share channels with the one before,
         // which has them (the states may be written over h0)
@@ -286,17 +277,101 @@ struct Place {
     }
 };
 
-// The block's place in the chain's order.
-__device__ __forceinline__ uint32_t next_tile(const Scan &p) {
-    if (!p.ticket) return blockIdx.x;
-    __shared__ uint32_t w;
-    if (threadIdx.x == 0)
-        w = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
+// A thread's vectors of its rows of a matrix; zeros behind row n.
+template <int DT, bool WIDE, int R>
+__device__ __forceinline__ void load_rows(const Scan &p, const void *m, int64_t ld, int64_t row,
+                                          int64_t c0, bool act, u32x4 (&raw)[R]) {
+    if (act && row + R <= p.n) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) raw[r] = load_vec<DT, WIDE>(m, ld, row + r, c0, p.d);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            raw[r] = u32x4{0, 0, 0, 0};
+            if (act && row + r < p.n) raw[r] = load_vec<DT, WIDE>(m, ld, row + r, c0, p.d);
+        }
+    }
+}
+
+// The slot of a lane of a wave (strips of 32-bit channels: of two lanes).
+template <int V>
+__device__ __forceinline__ int slot_of() {
+    return lane_id() & (kStripLanes * V - 1);
+}
+
+// The threads' maps of a tile, and what enters each thread's rows: each wave joins its
+// own row lanes, a slot to a lane, in row order or (BACK) from the last to the first.
+constexpr int kWaves = kBlock / kWave, kWaveRows = kRowLanes / kWaves;
+template <int V, bool BACK>
+struct Joint {
+    static constexpr int kSlots = kStripLanes * V;
+    Map part[kRowLanes][kSlots + kStripLanes];  // (rows a vector apart in the banks)
+    Map wave[kWaves][kSlots];
+    // the i-th row lane of a wave, and the i-th wave, in order
+    static __device__ __forceinline__ int lane_at(int wave, int i) {
+        return wave * kWaveRows + (BACK ? kWaveRows - 1 - i : i);
+    }
+    static __device__ __forceinline__ int wave_at(int i) { return BACK ? kWaves - 1 - i : i; }
+
+    __device__ __forceinline__ void put(int rl, int cl, const float *a, const float *c) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) part[rl][slot_at(q, cl)] = Map{a[q], c[q]};
+    }
+    // after the wave's put
+    __device__ __forceinline__ void join(int w) {
+        Team<1>::sync();
+        const int slot = slot_of<V>();
+        Map m = part[lane_at(w, 0)][slot];
+#pragma unroll
+        for (int i = 1; i < kWaveRows; ++i) m = then(m, part[lane_at(w, i)][slot]);
+        wave[w][slot] = m;
+    }
+    // after all waves' join
+    __device__ __forceinline__ Map total() const {
+        const int slot = slot_of<V>();
+        Map m = wave[wave_at(0)][slot];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) m = then(m, wave[wave_at(i)][slot]);
+        return m;
+    }
+    // h enters the tile: what enters each row lane of the wave, in the place of its map
+    __device__ __forceinline__ void spread(int w, float h) {
+        const int slot = slot_of<V>();
+#pragma unroll
+        for (int i = 0; i < kWaves - 1; ++i) {
+            if (wave_at(i) == w) break;
+            h = apply(wave[wave_at(i)][slot], h);
+        }
+#pragma unroll
+        for (int i = 0; i < kWaveRows; ++i) {
+            const int r = lane_at(w, i);
+            const Map m = part[r][slot];
+            part[r][slot].c = h;
+            h = apply(m, h);
+        }
+        Team<1>::sync();
+    }
+    __device__ __forceinline__ void get(int rl, int cl, float *h) const {
+#pragma unroll
+        for (int q = 0; q < V; ++q) h[q] = part[rl][slot_at(q, cl)].c;
+    }
+};
+
+// ----------------------------------------------------------------------------
+// the chain over tiles
+
+// A tile for the block, by one wave: its place in the chain's order.
+__device__ __forceinline__ uint32_t deal(const Scan &p) {
+    uint32_t w = blockIdx.x;
+    if (p.ticket) {
+        if (lane_id() == 0)
+            w = __hip_atomic_fetch_add(p.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        w = __builtin_amdgcn_readfirstlane(w);
+    }
     return w;
 }
 
-constexpr int kReach = 16;
+constexpr int kReach = 16;  // tiles that a hop of the chain passes
 constexpr int64_t kPatience = 200000000;  // ticks of the 100 MHz clock: 2 s
 constexpr int64_t kUneasy = 100000;       // 1 ms
 
@@ -333,87 +408,155 @@ __device__ __forceinline__ bool give_up(const Scan &p, int64_t t0) {
     return true;
 }
 
-// What enters the tile at `turn` of strip `strip`, whose map is m: by the first wave, a
-// slot to a lane.  A wait that lasts kPatience ends with NaN and a status.
+// Where a lane's words of the chain are; -1 of a lane without a slot.
 template <int V>
-__device__ __forceinline__ float chain(const Scan &p, int turn, int strip, Map m) {
-    constexpr int kSlots = Shared<V>::kSlots;
-    if (!p.ticket) return 0.0f;
-    const int64_t slots = (int64_t)p.strips * kSlots;
-    const int64_t at = (int64_t)turn * slots + (int64_t)strip * kSlots + slot_of<V>();
-    const bool first_of_slot = lane_id() < kSlots, next = turn < p.tiles - 1;
-    if (next && first_of_slot) post(p.total + at, word_of(m));
-    unsigned long long w[kReach - 1];
-    uint32_t h = 0;
-    bool late = false;
-    const int64_t t0 = now_ticks();
-    if (turn >= kReach) {
-        while (true) {
-            h = peek(p.leave + (at - kReach * slots));
-            if (!__any(h == ~0u)) break;
-            if ((late = give_up(p, t0))) break;
-            __builtin_amdgcn_s_sleep(4);
-        }
+struct Link {
+    int64_t slots, at;
+    bool mine;
+    __device__ __forceinline__ Link(const Scan &p, int turn, int strip) {
+        constexpr int kSlots = kStripLanes * V;
+        slots = (int64_t)p.strips * kSlots;
+        at = (int64_t)turn * slots + (int64_t)strip * kSlots + slot_of<V>();
+        mine = lane_id() < kSlots;
     }
-    const int maps = turn >= kReach ? kReach - 1 : turn;
-    while (!late) {
+};
+
+// What the waves of a block fetch of the chain: the maps of the kReach - 1 tiles before
+// its own, a third of them to each of three waves.
+template <int V>
+struct Fetched {
+    static constexpr int kEach = (kReach - 1) / 3;
+    static_assert(3 * kEach == kReach - 1, "thirds");
+    unsigned long long map[kReach - 1][kStripLanes * V];
+    float leave[kStripLanes * V];
+    int late;
+};
+template <int V>
+__device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, int third, Fetched<V> &f) {
+    constexpr int kEach = Fetched<V>::kEach;
+    if (!p.ticket) return;
+    const Link<V> l(p, turn, strip);
+    const int64_t t0 = now_ticks();
+    unsigned long long w[kEach];
+    while (true) {
         bool missing = false;
 #pragma unroll
-        for (int j = 0; j < kReach - 1; ++j) {
-            w[j] = 0;
-            if (j < maps) w[j] = peek(p.total + (at - (int64_t)(maps - j) * slots));
+        for (int j = 0; j < kEach; ++j) {
+            // (maps of no tile are not asked for: they are not applied)
+            const int back = third * kEach + j + 1;
+            w[j] = back <= turn ? peek(p.total + (l.at - back * l.slots)) : 0ull;
         }
 #pragma unroll
-        for (int j = 0; j < kReach - 1; ++j) missing |= w[j] == ~0ull;
+        for (int j = 0; j < kEach; ++j) missing |= w[j] == ~0ull;
         if (!__any(missing)) break;
-        late = give_up(p, t0);
-        __builtin_amdgcn_s_sleep(2);
+        if (__any(give_up(p, t0))) {
+            f.late = 1;
+            break;
+        }
+        __builtin_amdgcn_s_sleep(1);
     }
-    float enter = __uint_as_float(h);
-    if (late) {
-        enter = kNan;  // seen by whoever uses the result
-        if (p.status) *p.status = PDB_ERR_DEVICE;
-    } else {
 #pragma unroll
-        for (int j = 0; j < kReach - 1; ++j)
-            if (j < maps) enter = apply(map_of(w[j]), enter);
+    for (int j = 0; j < kEach; ++j) f.map[third * kEach + j][slot_of<V>()] = w[j];
+}
+
+// The block's own map, and the state behind the tile kReach before.
+template <int V>
+__device__ __forceinline__ void chain_wait(const Scan &p, int turn, int strip, Map m, Fetched<V> &f) {
+    if (!p.ticket) return;
+    const Link<V> l(p, turn, strip);
+    if (turn < p.tiles - 1 && l.mine) post(p.total + l.at, word_of(m));
+    uint32_t h = 0;
+    if (turn >= kReach) {
+        const int64_t t0 = now_ticks();
+        while (true) {
+            h = peek(p.leave + (l.at - kReach * l.slots));
+            if (!__any(h == ~0u)) break;
+            if (__any(give_up(p, t0))) {
+                f.late = 1;
+                break;
+            }
+            __builtin_amdgcn_s_sleep(1);
+        }
     }
-    if (turn + kReach < p.tiles && first_of_slot) post(p.leave + at, word_of(apply(m, enter)));
-    return enter;
+    f.leave[slot_of<V>()] = __uint_as_float(h);
+}
+// What enters the tile, from both, by every wave; `first`, one of them, publishes the state
+// behind the tile, whose map is m.  A wait that was given up ends with NaN and a status.
+template <int V>
+__device__ __forceinline__ float chain_end(const Scan &p, int turn, int strip, Map m, bool first,
+                                           const Fetched<V> &f) {
+    if (!p.ticket) return 0.0f;
+    float h = f.leave[slot_of<V>()];
+#pragma unroll
+    for (int j = kReach - 2; j >= 0; --j)
+        if (j < turn) h = apply(map_of(f.map[j][slot_of<V>()]), h);
+    if (f.late) {
+        h = kNan;  // seen by whoever uses the result
+        if (p.status) *p.status = PDB_ERR_DEVICE;
+    }
+    const Link<V> l(p, turn, strip);
+    if (first && turn + kReach < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
+    return h;
+}
+
+// ----------------------------------------------------------------------------
+// the kernels
+
+template <typename F>
+__device__ __forceinline__ void either(bool plain, F f) {
+    if (plain)
+        f(std::true_type());
+    else
+        f(std::false_type());
 }
 
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
-    constexpr int V = Elem<DT>::kVec;
-    __shared__ Shared<V> s;
-    const Place<DT, WIDE> at(p, next_tile(p), false);
-    int64_t lo, hi;
-    const bool plain =
-        find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.c0, at.own, at.act, p.h0, s.edges, lo, hi);
+    using S = Shape<DT, false>;
+    using At = Place<DT, WIDE, false>;
+    constexpr int V = S::V, R = S::kRows;
+    __shared__ Joint<V, false> s;
+    __shared__ Edges<S::kTileRows> e;
+    __shared__ Fetched<V> fetched;
+    const int wave = __builtin_amdgcn_readfirstlane(wave_in_block());
     check_starts(p);
-    float a[kRows][V], c[kRows][V];
-    auto local = [&](auto is_plain) {
-        constexpr bool kPlain = decltype(is_plain)::value;
-        u32x4 rx[kRows], rg[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            rx[r] = rg[r] = u32x4{0, 0, 0, 0};
-            if (at.act && (kPlain || at.row + r < p.n)) {
-                rx[r] = load_vec<DT, WIDE>(p.x, p.ldx, at.row + r, at.c0, p.d);
-                rg[r] = load_vec<DT, WIDE>(p.gate, p.ldg, at.row + r, at.c0, p.d);
-            }
+    if (wave == 0) {
+        const uint32_t w = deal(p);
+        const int32_t first = p.ticket ? 0 : first_edge(p, 0, S::kTileRows, true);
+        if (lane_id() == 0) {
+            e.dealt = w;
+            e.first = first;
+            fetched.late = 0;
         }
+    }
+    __syncthreads();
+    const At at(p, __builtin_amdgcn_readfirstlane(e.dealt));
+    const int32_t first = p.ticket ? p.first[at.tile] : e.first;
+    u32x4 rx[R], rg[R];
+    load_rows<DT, WIDE>(p, p.gate, p.ldg, at.row, at.c0, at.act, rg);
+    load_rows<DT, WIDE>(p, p.x, p.ldx, at.row, at.c0, at.act, rx);
+    bool plain = __builtin_amdgcn_readfirstlane(first) == kPlain;
+    if (!plain) {
+        if (wave == 1)
+            find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.strip, p.h0, first, e);
+        Team<kWaves>::sync_lds();
+        plain = plain_wave(e, at.r0, wave);
+    }
+    const int64_t lo = plain ? 0 : e.lo, hi = plain ? p.n : e.hi;
+    float a[R][V], c[R][V];
+    either(plain, [&](auto is_plain) {
+        constexpr bool kPlain = decltype(is_plain)::value;
         float ra[V], rc[V];
 #pragma unroll
         for (int q = 0; q < V; ++q) ra[q] = 1.0f, rc[q] = 0.0f;
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
+        for (int r = 0; r < R; ++r) {
             const int64_t row = at.row + r;
             if (kPlain || (row >= lo && row < hi)) {
                 float x[V], g[V];
                 unpack<DT>(rx[r], x);
                 unpack<DT>(rg[r], g);
-                const int begin = kPlain ? -1 : s.edges.begin[at.rl * kRows + r];
+                const int begin = kPlain ? -1 : e.begin[at.rl * R + r];
                 if (begin >= 0) {
                     if (at.act) load_row<V, WIDE>(p.h0, begin, at.c0, p.d, rc);
                     // now: when the states are written h0 may be gone
@@ -424,35 +567,37 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
                 }
 #pragma unroll
                 for (int q = 0; q < V; ++q) {
-                    const Gate w = open_gate(small_gate(g[q]));
+                    const Gate w = gate_of(g[q]);
                     rc[q] = __builtin_fmaf(w.f, rc[q], w.k * x[q]);
                     ra[q] *= w.f;
                 }
             }
 #pragma unroll
             for (int q = 0; q < V; ++q) a[r][q] = ra[q], c[r][q] = rc[q];
+            // a row after another: all of them unpacked at once would not fit
+            __builtin_amdgcn_sched_barrier(0);
         }
-    };
-    if (plain)
-        local(std::true_type());
+    });
+    s.put(at.rl, at.cl, a[R - 1], c[R - 1]);
+    s.join(wave);
+    __syncthreads();
+    const Map m = s.total();
+    if (wave == 0)
+        chain_wait<V>(p, at.turn, at.strip, m, fetched);
     else
-        local(std::false_type());
-    put_part(s, at.rl, at.cl, a[kRows - 1], c[kRows - 1]);
+        fetch_maps<V>(p, at.turn, at.strip, wave - 1, fetched);
     __syncthreads();
-    if (wave_in_block() == 0) {
-        const Map m = join_total<V, false>(s);
-        join_enter<V, false>(s, chain<V>(p, at.turn, at.strip, m));
-    }
-    __syncthreads();
+    s.spread(wave, chain_end<V>(p, at.turn, at.strip, m, wave == 0, fetched));
     float h[V];
-    get_enter(s, at.rl, at.cl, h);
-    auto finish = [&](auto is_plain) {
+    s.get(at.rl, at.cl, h);
+    if (!at.act) return;
+    either(plain, [&](auto is_plain) {
         constexpr bool kPlain = decltype(is_plain)::value;
         if (p.marks && at.row % PDB_SCAN_MARK == 0 && at.row < p.n &&
-            (kPlain || s.edges.begin[at.rl * kRows] < 0))
+            (kPlain || e.begin[at.rl * R] < 0))
             store_row<V, WIDE>(p.marks, at.row / PDB_SCAN_MARK, at.c0, p.d, at.own, h);
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
+        for (int r = 0; r < R; ++r) {
             const int64_t row = at.row + r;
             if (!kPlain && (row < lo || row >= hi)) continue;
             float out[V];
@@ -462,64 +607,93 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
                                 : apply(Map{a[r][q], c[r][q]}, h[q]);
             store_vec<DT, WIDE>(p.y, p.ldy, row, at.c0, p.d, at.own, out);
             if constexpr (!kPlain) {
-                const int end = s.edges.end[at.rl * kRows + r];
-                if (end >= 0 && p.state) store_row<V, WIDE>(p.state, end, at.c0, p.d, at.own, out);
+                const int end = e.end[at.rl * R + r];
+                if (end >= 0 && p.state)
+                    store_row<V, WIDE>(p.state, end, at.c0, p.d, at.own, out);
             }
         }
-    };
-    if (!at.act) return;
-    if (plain)
-        finish(std::true_type());
-    else
-        finish(std::false_type());
+    });
 }
 
 // The backward pass of a tile.  Going back, a row acts on e (what the rows behind it
 // ask of the state before them) as e -> f (dy + e); a row that ends a sequence takes
-// d_state in place of e.  The states come from the mark that the tile begins with.
+// d_state in place of e.  The states come from the mark that the tile begins with, so
+// that only e passes along the chain.
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
-    constexpr int V = Elem<DT>::kVec;
-    __shared__ Shared<V> s;
-    const Place<DT, WIDE> at(p, next_tile(p), true);
-    int64_t lo, hi;
-    const bool plain =
-        find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.c0, at.own, at.act, p.d_state, s.edges, lo, hi);
+__global__ __launch_bounds__(kBlock, 3) void k_scan_grad(Scan p) {
+    using S = Shape<DT, true>;
+    using At = Place<DT, WIDE, true>;
+    constexpr int V = S::V, R = S::kRows;
+    __shared__ Joint<V, false> forth;
+    __shared__ Joint<V, true> back;
+    __shared__ Edges<S::kTileRows> e;
+    __shared__ Fetched<V> fetched;
+    const int wave = __builtin_amdgcn_readfirstlane(wave_in_block());
     check_starts(p);
-    float w[kRows][V], x[kRows][V];
-    u32x4 ry[kRows];
-    auto inside = [&](int64_t row) { return row >= lo && row < hi; };
-    auto load = [&](auto is_plain) {
-        constexpr bool kPlain = decltype(is_plain)::value;
-        u32x4 rx[kRows], rg[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            rx[r] = rg[r] = ry[r] = u32x4{0, 0, 0, 0};
-            if (at.act && (kPlain || at.row + r < p.n)) {
-                rg[r] = load_vec<DT, WIDE>(p.gate, p.ldg, at.row + r, at.c0, p.d);
-                ry[r] = load_vec<DT, WIDE>(p.dy, p.lddy, at.row + r, at.c0, p.d);
-                rx[r] = load_vec<DT, WIDE>(p.x, p.ldx, at.row + r, at.c0, p.d);
-            }
+    if (wave == 0) {
+        const uint32_t w = deal(p);
+        const int32_t first = p.ticket ? 0 : first_edge(p, 0, S::kTileRows, true);
+        if (lane_id() == 0) {
+            e.dealt = w;
+            e.first = first;
+            fetched.late = 0;
         }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            float g[V];
-            unpack<DT>(rg[r], g);
-            unpack<DT>(rx[r], x[r]);
-#pragma unroll
-            for (int q = 0; q < V; ++q) w[r][q] = small_gate(g[q]);
-        }
-    };
-    // the thread's map of e, from its last row to its first
-    auto back = [&](auto is_plain) {
+    }
+    __syncthreads();
+    const At at(p, __builtin_amdgcn_readfirstlane(e.dealt));
+    const int32_t first = p.ticket ? p.first[at.tile] : e.first;
+    const int64_t ch = channel_of<V, WIDE>(p, at.strip, slot_of<V>(), false);
+    const float mark =
+        ch >= 0 && at.r0 < p.n ? p.marks_in[at.r0 / PDB_SCAN_MARK * p.d + ch] : 0.0f;
+    u32x4 rx[R], rg[R], ry[R];
+    load_rows<DT, WIDE>(p, p.gate, p.ldg, at.row, at.c0, at.act, rg);
+    load_rows<DT, WIDE>(p, p.x, p.ldx, at.row, at.c0, at.act, rx);
+    load_rows<DT, WIDE>(p, p.dy, p.lddy, at.row, at.c0, at.act, ry);
+    bool plain = __builtin_amdgcn_readfirstlane(first) == kPlain;
+    if (!plain) {
+        if (wave == 1)
+            find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.strip, p.d_state, first, e);
+        Team<kWaves>::sync_lds();
+        plain = plain_wave(e, at.r0, wave);
+    }
+    const int64_t lo = plain ? 0 : e.lo, hi = plain ? p.n : e.hi;
+    float f[R][V], k[R][V];
+    either(plain, [&](auto is_plain) {
         constexpr bool kPlain = decltype(is_plain)::value;
         float a[V], c[V];
 #pragma unroll
         for (int q = 0; q < V; ++q) a[q] = 1.0f, c[q] = 0.0f;
 #pragma unroll
-        for (int r = kRows - 1; r >= 0; --r) {
-            if (!kPlain && !inside(at.row + r)) continue;
-            const int end = kPlain ? -1 : s.edges.end[at.rl * kRows + r];
+        for (int r = 0; r < R; ++r) {
+            float x[V], g[V];
+            unpack<DT>(rx[r], x);
+            unpack<DT>(rg[r], g);
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                const Gate w = gate_of(g[q]);
+                f[r][q] = w.f;
+                k[r][q] = w.k;
+            }
+            if (!kPlain && (at.row + r < lo || at.row + r >= hi)) continue;
+            const int begin = kPlain ? -1 : e.begin[at.rl * R + r];
+            if (begin >= 0) {
+                if (at.act) load_row<V, WIDE>(p.h0, begin, at.c0, p.d, c);
+#pragma unroll
+                for (int q = 0; q < V; ++q) a[q] = -0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                c[q] = __builtin_fmaf(f[r][q], c[q], k[r][q] * x[q]);
+                a[q] *= f[r][q];
+            }
+        }
+        forth.put(at.rl, at.cl, a, c);
+#pragma unroll
+        for (int q = 0; q < V; ++q) a[q] = 1.0f, c[q] = 0.0f;
+#pragma unroll
+        for (int r = R - 1; r >= 0; --r) {
+            if (!kPlain && (at.row + r < lo || at.row + r >= hi)) continue;
+            const int end = kPlain ? -1 : e.end[at.rl * R + r];
             if (end >= 0) {
                 if (at.act) load_row<V, WIDE>(p.d_state, end, at.c0, p.d, c);
 #pragma unroll
@@ -529,109 +703,76 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan_grad(Scan p) {
             unpack<DT>(ry[r], dy);
 #pragma unroll
             for (int q = 0; q < V; ++q) {
-                const float f = open_gate(w[r][q]).f;
-                c[q] = f * (dy[q] + c[q]);
-                a[q] *= f;
+                c[q] = f[r][q] * (dy[q] + c[q]);
+                a[q] *= f[r][q];
             }
         }
-        put_part(s, at.rl, at.cl, a, c);
-    };
-    // the thread's map of h, and, with what enters, h_{t-1} - x_t in the place of x_t
-    auto forth = [&](auto is_plain, float *h, bool last) {
+        back.put(at.rl, at.cl, a, c);
+    });
+    forth.join(wave);
+    back.join(wave);
+    __syncthreads();
+    const Map m = back.total();
+    if (wave == 0)
+        chain_wait<V>(p, at.turn, at.strip, m, fetched);
+    else
+        fetch_maps<V>(p, at.turn, at.strip, wave - 1, fetched);
+    float h[V], g[V];
+    forth.spread(wave, mark);
+    forth.get(at.rl, at.cl, h);
+    __syncthreads();
+    back.spread(wave, chain_end<V>(p, at.turn, at.strip, m, wave == 0, fetched));
+    back.get(at.rl, at.cl, g);
+    if (!at.act) return;
+    either(plain, [&](auto is_plain) {
         constexpr bool kPlain = decltype(is_plain)::value;
-        float a[V];
+        float gap[R][V];  // h_{t-1} - x_t
 #pragma unroll
-        for (int q = 0; q < V; ++q) a[q] = 1.0f;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            if (!kPlain && !inside(at.row + r)) continue;
-            const int begin = kPlain ? -1 : s.edges.begin[at.rl * kRows + r];
-            if (begin >= 0) {
-                if (at.act) load_row<V, WIDE>(p.h0, begin, at.c0, p.d, h);
-#pragma unroll
-                for (int q = 0; q < V; ++q) a[q] = -0.0f;
-            }
+        for (int r = 0; r < R; ++r) {
+            if (!kPlain && (at.row + r < lo || at.row + r >= hi)) continue;
+            const int begin = kPlain ? -1 : e.begin[at.rl * R + r];
+            if (begin >= 0) load_row<V, WIDE>(p.h0, begin, at.c0, p.d, h);
+            float x[V];
+            unpack<DT>(rx[r], x);
 #pragma unroll
             for (int q = 0; q < V; ++q) {
-                const Gate g = open_gate(w[r][q]);
-                const float now = __builtin_fmaf(g.f, h[q], g.k * x[r][q]);
-                if (last) x[r][q] = h[q] - x[r][q];
-                h[q] = now;
-                a[q] *= g.f;
+                gap[r][q] = h[q] - x[q];
+                h[q] = __builtin_fmaf(f[r][q], h[q], k[r][q] * x[q]);
             }
         }
-        if (!last) put_part(s, at.rl, at.cl, a, h);
-    };
-    auto both = [&](auto f) {
-        if (plain)
-            f(std::true_type());
-        else
-            f(std::false_type());
-    };
-    both(load);
-    {
-        float h[V];
 #pragma unroll
-        for (int q = 0; q < V; ++q) h[q] = 0.0f;
-        both([&](auto t) { forth(t, h, false); });
-        __syncthreads();
-        if (wave_in_block() == 0) {
-            // the mark, by slots
-            const int slot = slot_of<V>();
-            float m = 0.0f;
-            const int64_t cs = ((int64_t)at.strip * kStripLanes + slot / V) * V;
-            const int64_t ch = (WIDE ? min(cs, p.d - V) : cs) + slot % V;
-            if (cs < p.d && ch < p.d && at.r0 < p.n)
-                m = p.marks_in[at.r0 / PDB_SCAN_MARK * p.d + ch];
-            join_enter<V, false>(s, m);
-        }
-        __syncthreads();
-        get_enter(s, at.rl, at.cl, h);
-        both([&](auto t) { forth(t, h, true); });
-        __syncthreads();
-    }
-    both(back);
-    __syncthreads();
-    if (wave_in_block() == 0) {
-        const Map m = join_total<V, true>(s);
-        join_enter<V, true>(s, chain<V>(p, at.turn, at.strip, m));
-    }
-    __syncthreads();
-    if (!at.act) return;
-    float e[V];
-    get_enter(s, at.rl, at.cl, e);
-    both([&](auto is_plain) {
-        constexpr bool kPlain = decltype(is_plain)::value;
-#pragma unroll
-        for (int r = kRows - 1; r >= 0; --r) {
-            if (!kPlain && !inside(at.row + r)) continue;
-            const int end = kPlain ? -1 : s.edges.end[at.rl * kRows + r];
-            if (end >= 0) load_row<V, WIDE>(p.d_state, end, at.c0, p.d, e);
+        for (int r = R - 1; r >= 0; --r) {
+            if (!kPlain && (at.row + r < lo || at.row + r >= hi)) continue;
+            const int end = kPlain ? -1 : e.end[at.rl * R + r];
+            if (end >= 0) load_row<V, WIDE>(p.d_state, end, at.c0, p.d, g);
             float dy[V], dx[V], dg[V];
             unpack<DT>(ry[r], dy);
 #pragma unroll
             for (int q = 0; q < V; ++q) {
-                const Gate g = open_gate(w[r][q]);
-                const float t = dy[q] + e[q];
-                dx[q] = g.k * t;
-                dg[q] = t * x[r][q] * (g.f * g.k);
-                e[q] = g.f * t;
+                const float t = dy[q] + g[q];
+                dx[q] = k[r][q] * t;
+                g[q] = f[r][q] * t;
+                dg[q] = gap[r][q] * (k[r][q] * g[q]);
             }
             store_vec<DT, WIDE>(p.y, p.ldy, at.row + r, at.c0, p.d, at.own, dx);
             store_vec<DT, WIDE>(p.dgate, p.lddg, at.row + r, at.c0, p.d, at.own, dg);
             if constexpr (!kPlain) {
-                const int begin = s.edges.begin[at.rl * kRows + r];
-                if (begin >= 0 && p.state) store_row<V, WIDE>(p.state, begin, at.c0, p.d, at.own, e);
+                const int begin = e.begin[at.rl * R + r];
+                if (begin >= 0 && p.state)
+                    store_row<V, WIDE>(p.state, begin, at.c0, p.d, at.own, g);
             }
         }
     });
 }
 
-// A chain's words before it begins.
-__global__ __launch_bounds__(kBlock) void k_scan_clear(uint32_t *words, int64_t count) {
-    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < count;
-         i += (int64_t)gridDim.x * kBlock)
-        words[i] = i == 0 ? 0u : ~0u;
+// A chain's words before it begins, and the tiles' first edges: a tile to a wave.
+__global__ __launch_bounds__(kBlock) void k_scan_clear(Scan p, int64_t words, int rows) {
+    const int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x, all = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = at; i < words; i += all) p.ticket[i] = i == 0 ? 0u : ~0u;
+    for (int64_t t = at / kWave; t < p.tiles; t += all / kWave) {
+        const int32_t f = first_edge(p, t * rows, (t + 1) * rows, t == p.tiles - 1);
+        if (lane_id() == 0) p.first[t] = f;
+    }
 }
 
 // Sequences of one row each: no state but the one that is given passes along.
@@ -651,7 +792,7 @@ __global__ __launch_bounds__(kBlock) void k_scan_step(Scan p, int64_t vecs) {
         store_row<V, WIDE>(p.marks, i / PDB_SCAN_MARK, c0, p.d, own, h);
 #pragma unroll
     for (int q = 0; q < V; ++q) {
-        const Gate k = open_gate(small_gate(g[q]));
+        const Gate k = gate_of(g[q]);
         h[q] = __builtin_fmaf(k.f, h[q], k.k * x[q]);
     }
     store_vec<DT, WIDE>(p.y, p.ldy, i, c0, p.d, own, h);
@@ -668,19 +809,23 @@ __global__ __launch_bounds__(kBlock) void k_scan_none(const float *from, float *
 struct Cut {
     int64_t tiles, strips, slots;  // slots: of a tile
 };
-Cut cut_of(int64_t n, int64_t d, int dtype) {
-    const int64_t v = 16 / dtype_size(dtype), strips = cdiv(std::max<int64_t>(d, 1), kStripLanes * v);
-    return {std::max<int64_t>(cdiv(n, kTileRows), 1), strips, strips * kStripLanes * v};
+Cut cut_of(int64_t n, int64_t d, int dtype, bool back) {
+    const int64_t v = 16 / dtype_size(dtype), strips = cdiv(std::max<int64_t>(d, 1), kStripLanes * v),
+                  rows = kRowLanes * (back ? 4 : 8);
+    return {std::max<int64_t>(cdiv(n, rows), 1), strips, strips * kStripLanes * v};
 }
 // The chain's words: the counter (in a line of its own), the maps, the states.
 int64_t scan_words(const Cut &c) { return kAlign / 4 + c.tiles * c.slots * 3; }
+// ... and the tiles' first edges.
+int64_t scan_bytes(const Cut &c) { return align_up((scan_words(c) + c.tiles) * 4); }
 size_t scan_ws_bytes(int64_t n, int64_t d) {
-    return (size_t)align_up(scan_words(cut_of(n, d, PDB_BF16)) * 4);  // the widest strips
+    // the most tiles, the widest strips
+    return (size_t)scan_bytes(cut_of(n, d, PDB_BF16, true));
 }
 
 template <bool GRAD>
 int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
-    const Cut cut = cut_of(p.n, p.d, dtype);
+    const Cut cut = cut_of(p.n, p.d, dtype, GRAD);
     if (p.n == 0 && !p.starts) {
         if (!p.state) return PDB_OK;
         k_scan_none<<<grid_for((int64_t)p.b * p.d, kBlock, 4096), kBlock, 0, stream>>>(
@@ -696,6 +841,7 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
         p.ticket = static_cast<uint32_t *>(ws);
         p.total = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + kAlign);
         p.leave = reinterpret_cast<uint32_t *>(p.total + cut.tiles * cut.slots);
+        p.first = reinterpret_cast<int32_t *>(p.ticket + scan_words(cut));
     }
     return with_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
@@ -711,7 +857,8 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
             }
             if (p.ticket) {
                 const int64_t words = scan_words(cut);
-                k_scan_clear<<<grid_for(words, kBlock * 4, 2048), kBlock, 0, stream>>>(p.ticket, words);
+                k_scan_clear<<<grid_for(std::max(words / 4, cut.tiles * kWave), kBlock, 2048), kBlock, 0,
+                               stream>>>(p, words, Shape<DT, GRAD>::kTileRows);
             }
             if constexpr (GRAD)
                 k_scan_grad<DT, W><<<grid, kBlock, 0, stream>>>(p);
