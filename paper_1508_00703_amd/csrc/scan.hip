@@ -53,9 +53,11 @@ struct Gate {
     float f, k;
 };
 __device__ __forceinline__ Gate gate_of(float g) {
-    const float t = exp2_raw(-fabsf(g) * kLog2e);
-    const float l = __builtin_amdgcn_rcpf(1.0f + t), s = t * l;
-    return g < 0.0f ? Gate{s, l} : Gate{l, s};
+    const float t = exp2_raw(g * -kLog2e);
+    const float f = __builtin_amdgcn_rcpf(1.0f + t);
+    // (an infinite t: f = 0 and t f no number, of which fmin takes the 1; a gate that is no
+    // number stays one in f)
+    return {f, fminf(t * f, 1.0f)};
 }
 
 struct Scan {
