@@ -2,28 +2,38 @@
 // numbers; with nothing drafted, the drawing of a token (gfx950, wave64).
 //
 // The answers are choices: whether u q(x) < p(x), and where a running sum over the
-// vocabulary passes u R.  In binary32 a sum over 131,072 entries is off by 1e-6 and
-// more, as much as many an entry has; so exponentials, probabilities and sums are in
-// binary64, which gfx950's vector unit multiplies and adds at half the rate of binary32.
+// vocabulary passes u R.  In binary32 a sum over 131,072 entries is off by 1e-6 and more,
+// as much as many an entry has; so what an answer hangs on is in binary64, which the
+// vector unit multiplies and adds at half the rate of binary32, and the rest is not:
 //
-// Three launches: every row's maximum and sum (rows in parts where they are few); then,
-// for the row at which each sequence stopped, the weights' sum of every chunk of
-// kChunk entries; then the chunk and the entry in it that the random number picks.
+// 1. every row's maximum and sum, one pass at the rate of memory: exponentials in
+//    binary32, sums of 32 of them added in binary64.  The sums are within kNear of the
+//    true ones; the few tokens that stand nearer than that to the bar get them exactly.
+// 2. of the row at which each sequence stopped, chunk by chunk in binary64: the sums of
+//    e_p and e_q (exp of logits below the row's maximum), and those over the entries that
+//    p has more of, e_p > r e_q with r = S_p / S_q: by step 1's r, since their exact r is
+//    known only behind this step.  Entries within kNear of it are put aside.
+// 3. with S_p and S_q, a chunk's residual is A - r B and what the entries put aside leave
+//    (a chunk of many of them is done again); the chunk that the random number picks is
+//    run through entry by entry.
+// Without drafted tokens step 1 is left out: chunks have maxima of their own.
 #include "pdb_softmax.h"
 
 namespace pdbk {
 namespace {
 
-constexpr int kEach = 16;               // consecutive entries of a thread
-constexpr int kChunk = kBlock * kEach;  // 4096
+// Consecutive entries of a thread: a chunk is kBlock times as many.  Drawing alone, without
+// drafted tokens, is bound by the exponentials (256 rows of 131,072: 43 us with 16, 54 with
+// 8); behind a draft it is latency (1 row of four: 22 us with 8, 24 with 16).
+constexpr int each_of(int32_t k) { return k == 0 ? 16 : 8; }
 constexpr double kLowest = -700.0;      // powers below this count as 0
+// What step 1's sums may be off by, relatively, two rows of them: an exponential's power
+// by 2 units of 2^-24 of its size (c = log2(e) / T and the product are rounded; on average
+// over a row the size is below 40), itself by 2, 32 added one to another, and the joins.
+constexpr double kNear = 0x1p-15;
 
-// e^y for y <= 0 (0 below kLowest, NaN of NaN): 2^n 2^f by the series of e^(f ln 2)
-// through f^12, |f| <= 1/2; what is left out is below 2e-16.
-__device__ __forceinline__ double exp_f64(double y) {
-    const double t = y * 0x1.71547652b82fep+0;
-    const double n = __builtin_rint(t);
-    const double f = t - n;
+// 2^f by the series of e^(f ln 2) through f^12, |f| <= 1/2; what is left out is below 2e-16.
+__device__ __forceinline__ double exp2_series(double f) {
     double r = 0x1.c3bd650fc2983p-36;
     r = fma(r, f, 0x1.e8cac7351bb22p-32);
     r = fma(r, f, 0x1.e4cf5158b8ec7p-28);
@@ -36,9 +46,39 @@ __device__ __forceinline__ double exp_f64(double y) {
     r = fma(r, f, 0x1.c6b08d704a0bfp-5);
     r = fma(r, f, 0x1.ebfbdff82c58ep-3);
     r = fma(r, f, 0x1.62e42fefa39efp-1);
-    r = fma(r, f, 1.0);
-    return y < kLowest ? 0.0 : __builtin_amdgcn_ldexp(r, (int)n);
+    return fma(r, f, 1.0);
 }
+// e^y for y <= 0 (0 below kLowest, NaN of NaN)
+__device__ __forceinline__ double exp_f64(double y) {
+    const double t = y * 0x1.71547652b82fep+0;
+    const double n = __builtin_rint(t);
+    return y < kLowest ? 0.0 : __builtin_amdgcn_ldexp(exp2_series(t - n), (int)n);
+}
+// The same of (z - m) / T, with the powers 2^(j / 64) in LDS: t = n + j / 64 + f, |f| <=
+// 1/128, and five terms of the series (what is left out is below 5e-14).  Half of
+// exp_f64's operations in binary64.
+struct Powers {
+    double at[64];
+    __device__ __forceinline__ void fill() {  // then a barrier
+        const int t = threadIdx.x;
+        if (t < 64) at[t] = t < 33 ? exp2_series(t / 64.0) : 2.0 * exp2_series((t - 64) / 64.0);
+    }
+    // by: 64 log2(e) / T
+    __device__ __forceinline__ double exp(double z, double m, double by) const {
+        const double t = (z - m) * by;
+        const double shifted = t + 0x1.8p52;  // t's nearest whole number is in its low bits
+        const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, shifted);
+        const double f = t - (shifted - 0x1.8p52);
+        double r = 0x1.3b2ab6fba4e77p-31;
+        r = fma(r, f, 0x1.c6b08d704a0bfp-23);
+        r = fma(r, f, 0x1.ebfbdff82c58ep-15);
+        r = fma(r, f, 0x1.62e42fefa39efp-7);
+        r = fma(r, f, 1.0) * at[k & 63];
+        // (2^-1010 and up: the power goes into the exponent's bits)
+        const int hi = __double2hiint(r) + ((k >> 6) << 20);
+        return t < kLowest * 0x1.71547652b82fep+6 ? 0.0 : __hiloint2double(hi, __double2loint(r));
+    }
+};
 
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
@@ -65,26 +105,31 @@ __device__ __forceinline__ void raise(Sum &t, double m, double inv_t) {
         t.m = m;
     }
 }
-__device__ __forceinline__ double weight(float z, double m, double inv_t) {
-    return exp_f64(((double)z - m) * inv_t);
-}
-
+struct Choice {
+    double mp, mq;   // the largest logits of the rows p and q
+    double r;        // S_p / S_q as step 1 has them; 0 without q
+    int32_t at, x;   // where the sequence stopped; the refused token, -1 if none
+};
+struct Chunk {
+    double m, sp, sq;  // m: what the powers of p are below
+    double a, b;       // of the entries with e_p > r e_q: the sums of e_p and of e_q
+    int32_t near, pad;  // entries put aside; kAgain: the chunk is to be done again
+};
+constexpr int kAside = 8, kAgain = -1;
 struct Verify {
     const void *target, *draft, *tokens;
     int64_t ldt, ldq, v;
     int32_t b, k, index;
     const float *u;
-    double inv_t;
+    double inv_t, by;  // 1 / T, 64 log2(e) / T
+    float c;           // log2(e) / T
     int32_t *out, *accepted, *status;
-    Parts cut;
+    int32_t parts, vecs;  // of a row in step 1; vectors of a part
     int64_t chunks;
     Sum *part;       // [rows][parts]: the targets' rows, then the drafts'
-    struct Choice *choice;  // [b]
-    double2 *mass;   // [b][chunks]: of max(p - q, 0), and of p
-};
-struct Choice {
-    double mp, ip, mq, iq;  // maximum and 1 / sum of the rows p and q
-    int32_t at, x;          // where the sequence stopped; the refused token, -1 if none
+    Choice *choice;  // [b]
+    Chunk *chunk;    // [b][chunks]
+    double2 *aside;  // [b][chunks][kAside]: e_p and e_q of entries put aside
 };
 
 // How many tokens a sequence has, the same in every lane.
@@ -93,13 +138,16 @@ __device__ __forceinline__ int drafted(const Verify &p, int64_t i) {
     if (lane_id() < p.k)
         bad = read_token(p.tokens, p.index, i * p.k + lane_id(), p.v, nullptr) < 0;
     const unsigned long long none = __ballot(bad);
-    return none ? __ffsll((unsigned long long)none) - 1 : p.k;
+    return none ? __ffsll(none) - 1 : p.k;
 }
+
+// ----------------------------------------------------------------------------
+// step 1
 
 template <int DT>
 __global__ __launch_bounds__(kBlock) void k_verify_sums(Verify p) {
-    constexpr int V = Elem<DT>::kVec;
-    const Work w(blockIdx.x, p.cut.parts);
+    constexpr int V = Elem<DT>::kVec, kW = kBlock / kWave;
+    const Work w(blockIdx.x, p.parts);
     const int64_t targets = (int64_t)p.b * (p.k + 1);
     const bool of_draft = w.i >= targets;
     const int64_t r = of_draft ? w.i - targets : w.i;
@@ -109,59 +157,54 @@ __global__ __launch_bounds__(kBlock) void k_verify_sums(Verify p) {
     if (of_draft ? j >= have : j > have) return;
     const char *row = of_draft ? elem_at<DT>(p.draft, r * p.ldq) : elem_at<DT>(p.target, r * p.ldt);
     const int full = (int)(p.v / V), rem = (int)(p.v - (int64_t)full * V);
-    const int first = w.part * p.cut.vecs;
-    const int end = std::min<int64_t>(full, (int64_t)first + p.cut.vecs);
-    const bool last = w.part == p.cut.parts - 1;
-    float m = -FLT_MAX;
+    const int first = w.part * p.vecs, end = min(full, first + p.vecs);
+    Stat t = {-FLT_MAX, 0.0f, 0.0f};  // of a tile
     double s = 0.0;
+    auto raise_to = [&](float m) {
+        Stat f = {t.m, 1.0f, 0.0f};
+        rescale(f, m, p.c);
+        s *= (double)f.s;
+        t.m = m;
+    };
     for (int q = first; q < end; q += kTileVecs * kBlock) {
-        const Tile tile = load_tile<DT, kBlock / kWave>(row, q, end);
+        Tile tile = load_tile<DT, kW>(row, q, end);
         float all = kNegInf;
 #pragma unroll
         for (int u = 0; u < kTileVecs; ++u) all = fmaxf(all, vec_max<DT>(tile.r[u]));
-        if (__any(all > m)) {
-            const float up = fmaxf(m, wave_max_f32(all));
-            s *= exp_f64(((double)m - (double)up) * p.inv_t);
-            m = up;
-        }
-#pragma unroll
-        for (int u = 0; u < kTileVecs; ++u) {
-            float x[V];
-            unpack<DT>(tile.r[u], x);
-#pragma unroll
-            for (int e = 0; e < V; ++e) s += weight(x[e], m, p.inv_t);
-        }
+        if (__any(all > t.m)) raise_to(fmaxf(t.m, wave_max_f32(all)));
+        t.s = 0.0f;
+        add_vecs<DT, false>(tile.r, p.c, t);
+        s += (double)t.s;
     }
-    if (last && wave_in_block() == 0) {
-        const float z = tail_elem<DT, kBlock / kWave>(row, full, rem);
-        if (__any(z > m)) {
-            const float up = fmaxf(m, wave_max_f32(z));
-            s *= exp_f64(((double)m - (double)up) * p.inv_t);
-            m = up;
-        }
-        s += weight(z, m, p.inv_t);
+    if (w.part == p.parts - 1 && wave_in_block() == 0) {
+        const float z = tail_elem<DT, kW>(row, full, rem);
+        if (__any(z > t.m)) raise_to(fmaxf(t.m, wave_max_f32(z)));
+        s += (double)exp2_raw(power_of(z, t.m, p.c));
     }
-    __shared__ Sum part[kBlock / kWave];
-    s = wave_sum_f64(s);
-    if (lane_id() == 0) part[wave_in_block()] = Sum{m, s};
+    __shared__ Sum part[kW];
+    s = wave_sum_f64(s) * exp2_series(-(double)shift_of(t.m, p.c));
+    if (lane_id() == 0) part[wave_in_block()] = Sum{t.m, s};
     __syncthreads();
     if (threadIdx.x == 0) {
-        Sum t = part[0];
-        for (int k = 1; k < kBlock / kWave; ++k) {
-            Sum o = part[k];
-            const double top = fmax(t.m, o.m);
-            raise(t, top, p.inv_t);
+        Sum a = part[0];
+        for (int i = 1; i < kW; ++i) {
+            Sum o = part[i];
+            const double top = fmax(a.m, o.m);
+            raise(a, top, p.inv_t);
             raise(o, top, p.inv_t);
-            t.s += o.s;
+            a.s += o.s;
         }
-        p.part[w.i * p.cut.parts + w.part] = t;
+        p.part[w.i * p.parts + w.part] = a;
     }
 }
+
+// ----------------------------------------------------------------------------
+// step 2
 
 // A row's maximum and sum from its parts', the same in every lane.
 __device__ __forceinline__ Sum join_sums(const Verify &p, int64_t row) {
     Sum t = {-FLT_MAX, 0.0};
-    if (lane_id() < p.cut.parts) t = p.part[row * p.cut.parts + lane_id()];
+    if (lane_id() < p.parts) t = p.part[row * p.parts + lane_id()];
     double m = t.m;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
@@ -169,110 +212,219 @@ __device__ __forceinline__ Sum join_sums(const Verify &p, int64_t row) {
     return {m, wave_sum_f64(t.s)};
 }
 
+__device__ __forceinline__ double block_sum_f64(double v) {
+    __shared__ double s[kBlock / kWave];
+    v = wave_sum_f64(v);
+    if (lane_id() == 0) s[wave_in_block()] = v;
+    __syncthreads();
+    v = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    return v;
+}
+static_assert(kBlock == 4 * kWave, "four waves");
+
+// The exact sum of a row, by the block.
+template <int DT>
+__device__ double exact_sum(const Verify &p, const char *row, double m, const Powers &e) {
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < p.v; i += kBlock)
+        s += e.exp((double)load1<DT>(row, i), m, p.by);
+    return block_sum_f64(s);
+}
+
 // Where sequence i stops, by one block.
 template <int DT>
-__device__ __forceinline__ Choice choose(const Verify &p, int64_t i) {
+__device__ __forceinline__ Choice choose(const Verify &p, int64_t i, const Powers &e) {
     __shared__ Sum st[PDB_MAX_DRAFT + 1], sq[PDB_MAX_DRAFT];
-    __shared__ Choice c;
-    const int have = drafted(p, i), wave = wave_in_block();
+    __shared__ unsigned long long stops, nears;
+    const int have = drafted(p, i), wave = wave_in_block(), j = lane_id();
     const int64_t targets = (int64_t)p.b * (p.k + 1);
-    for (int j = wave; j <= have; j += kBlock / kWave) {
-        const Sum s = join_sums(p, i * (p.k + 1) + j);
-        if (lane_id() == 0) st[j] = s;
-        if (j < have && p.draft) {
-            const Sum d = join_sums(p, targets + i * p.k + j);
-            if (lane_id() == 0) sq[j] = d;
+    for (int r = wave; r <= have; r += kBlock / kWave) {
+        const Sum s = join_sums(p, i * (p.k + 1) + r);
+        if (lane_id() == 0) st[r] = s;
+        if (r < have && p.draft) {
+            const Sum d = join_sums(p, targets + i * p.k + r);
+            if (lane_id() == 0) sq[r] = d;
         }
     }
     __syncthreads();
-    if (wave == 0) {
-        const int j = lane_id();
-        bool stop = j >= have;
-        int32_t x = -1;
+    // a position to a lane of the first wave: whether it is refused, and whether step 1's
+    // sums leave that open
+    auto decide = [&](bool exact) {
+        bool stop = j >= have, near = false;
         if (!stop) {
-            x = read_token(p.tokens, p.index, i * p.k + j, p.v, nullptr);
+            const int32_t x = read_token(p.tokens, p.index, i * p.k + j, p.v, nullptr);
             const float z = load1<DT>(p.target, (i * (p.k + 1) + j) * p.ldt + x);
-            const double px = weight(z, st[j].m, p.inv_t) / st[j].s;
+            const double px = e.exp((double)z, st[j].m, p.by) / st[j].s;
             double qx = 1.0;
             if (p.draft) {
-                const float zq = load1<DT>(p.draft, (i * p.k + j) * p.ldq + x);
-                qx = sq[j].s == 0.0 ? 0.0 : weight(zq, sq[j].m, p.inv_t) / sq[j].s;
+                const float y = load1<DT>(p.draft, (i * p.k + j) * p.ldq + x);
+                qx = sq[j].s == 0.0 ? 0.0 : e.exp((double)y, sq[j].m, p.by) / sq[j].s;
             }
-            stop = !((double)p.u[i * (p.k + 1) + j] * qx < px);
+            const double bar = (double)p.u[i * (p.k + 1) + j] * qx;
+            stop = !(bar < px);
+            near = px > 0.0 && fabs(px - bar) <= kNear * px;
         }
-        const unsigned long long stops = __ballot(stop);
-        const int at = stops ? __ffsll((unsigned long long)stops) - 1 : have;
-        x = __shfl(x, at & (kWave - 1));
+        const unsigned long long s = __ballot(stop), n = __ballot(near);
         if (j == 0) {
-            c.at = at;
-            c.x = at < have ? x : -1;
-            const Sum s = st[at];
-            c.mp = s.m;
-            c.ip = s.s == 0.0 ? 0.0 : 1.0 / s.s;
-            c.mq = c.iq = 0.0;
-            if (at < have && p.draft) {
-                c.mq = sq[at].m;
-                c.iq = sq[at].s == 0.0 ? 0.0 : 1.0 / sq[at].s;
-            }
+            if (!exact) nears = n;
+            stops = s;
+        }
+    };
+    if (wave == 0) decide(false);
+    __syncthreads();
+    // those nearer than step 1 can tell, as far as they come before the first refused
+    while (true) {
+        const unsigned long long n = nears, before = stops ? (stops & -stops) * 2 - 1 : ~0ull;
+        if (!(n & before)) break;
+        const int r = __ffsll(n & before) - 1;
+        const double s = exact_sum<DT>(p, elem_at<DT>(p.target, (i * (p.k + 1) + r) * p.ldt), st[r].m, e);
+        const double d = p.draft ? exact_sum<DT>(p, elem_at<DT>(p.draft, (i * p.k + r) * p.ldq), sq[r].m, e)
+                                 : 0.0;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            st[r].s = s;
+            if (p.draft) sq[r].s = d;
+            nears = n & ~(1ull << r);
+        }
+        __syncthreads();
+        if (wave == 0) decide(true);
+        __syncthreads();
+    }
+    // (with k = 64 drafted tokens there is no lane behind the last)
+    const int at = stops ? __ffsll(stops) - 1 : have;
+    Choice c = {st[at].m, 0.0, 0.0, at, -1};
+    if (at < have) {
+        c.x = read_token(p.tokens, p.index, i * p.k + at, p.v, nullptr);
+        if (p.draft) {
+            c.mq = sq[at].m;
+            c.r = sq[at].s == 0.0 ? 0.0 : st[at].s / sq[at].s;
         }
     }
     __syncthreads();
     return c;
 }
 
-// A thread's kEach entries from e0 on: p, and what a refused token leaves of it.
-template <int DT>
-__device__ __forceinline__ void weights(const Verify &p, const Choice &c, int64_t i, int64_t e0,
-                                        double *wp, double *wr) {
-    constexpr int V = Elem<DT>::kVec;
+// A thread's E logits from e0 on of the rows that a sequence stopped at, -inf behind
+// the row's end and in y where there is no q.
+template <int DT, int E>
+__device__ __forceinline__ void load_each(const Verify &p, const Choice &c, int64_t i, int64_t e0,
+                                          float *x, float *y) {
+    static_assert(E % Elem<DT>::kVec == 0, "whole vectors");
     const char *zt = elem_at<DT>(p.target, (i * (p.k + 1) + c.at) * p.ldt);
     const bool has_q = c.x >= 0 && p.draft;
     const char *zq = has_q ? elem_at<DT>(p.draft, (i * p.k + c.at) * p.ldq) : nullptr;
-    float x[kEach], y[kEach];
-    if (e0 + kEach <= p.v) {
-        load_elems<DT, kEach>(zt, e0, x);
-        if (has_q) load_elems<DT, kEach>(zq, e0, y);
+    if (e0 + E <= p.v) {
+        load_elems<DT, E>(zt, e0, x);
+        if (has_q) load_elems<DT, E>(zq, e0, y);
     } else {
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) {
+        for (int q = 0; q < E; ++q) {
             x[q] = e0 + q < p.v ? load1<DT>(zt, e0 + q) : kNegInf;
-            y[q] = has_q && e0 + q < p.v ? load1<DT>(zq, e0 + q) : kNegInf;
+            if (has_q) y[q] = e0 + q < p.v ? load1<DT>(zq, e0 + q) : kNegInf;
         }
     }
-    static_assert(kEach % V == 0, "whole vectors");
+    if (!has_q) {
 #pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        // (a row of nothing but -inf: 1 / sum is 0, and no weight is above 0)
-        wp[q] = weight(x[q], c.mp, p.inv_t) * c.ip;
-        double r = 0.0;
-        if (c.x >= 0) {
-            r = has_q ? wp[q] - weight(y[q], c.mq, p.inv_t) * c.iq : (e0 + q == c.x ? 0.0 : wp[q]);
-            r = r > 0.0 ? r : 0.0;
-        }
-        wr[q] = r;
+        for (int q = 0; q < E; ++q) y[q] = kNegInf;
     }
 }
 
 template <int DT>
-__global__ __launch_bounds__(kBlock) void k_verify_mass(Verify p) {
+__global__ __launch_bounds__(kBlock) void k_verify_choose(Verify p) {
+    __shared__ Powers e;
+    e.fill();
+    __syncthreads();
+    const Choice c = choose<DT>(p, blockIdx.x, e);
+    if (threadIdx.x == 0) p.choice[blockIdx.x] = c;
+}
+
+// FUSED: the blocks of a sequence each find where it stops; else k_verify_choose has.
+template <int DT, int E, bool FUSED>
+__global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
+    constexpr int kChunk = kBlock * E;
+    __shared__ Powers e;
+    __shared__ int counts[kBlock / kWave];
+    __shared__ double sums[kBlock / kWave][4];
+    __shared__ float tops[kBlock / kWave];
     const int64_t i = blockIdx.x / p.chunks, k = blockIdx.x - i * p.chunks;
-    const Choice c = choose<DT>(p, i);
-    if (k == 0 && threadIdx.x == 0) p.choice[i] = c;
-    double wp[kEach], wr[kEach], sp = 0.0, sr = 0.0;
-    weights<DT>(p, c, i, k * kChunk + threadIdx.x * kEach, wp, wr);
+    const int64_t e0 = k * kChunk + threadIdx.x * E;
+    e.fill();
+    __syncthreads();
+    Choice c = {0.0, 0.0, 0.0, 0, -1};
+    float x[E], y[E];
+    if (p.k > 0) {
+        if constexpr (FUSED)
+            c = choose<DT>(p, i, e);
+        else
+            c = p.choice[i];
+        load_each<DT, E>(p, c, i, e0, x, y);
+    } else {
+        load_each<DT, E>(p, c, i, e0, x, y);
+        float top = -FLT_MAX;
 #pragma unroll
-    for (int q = 0; q < kEach; ++q) sp += wp[q], sr += wr[q];
-    sp = wave_sum_f64(sp);
-    sr = wave_sum_f64(sr);
-    __shared__ double2 s[kBlock / kWave];
-    if (lane_id() == 0) s[wave_in_block()] = double2{sr, sp};
+        for (int q = 0; q < E; ++q) top = fmaxf(top, x[q]);
+        top = wave_max_f32(top);
+        if (lane_id() == 0) tops[wave_in_block()] = top;
+        __syncthreads();
+        c.mp = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    }
+    if ((FUSED || p.k == 0) && k == 0 && threadIdx.x == 0) p.choice[i] = c;
+    const bool has_q = c.x >= 0 && p.draft;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};  // e_p, e_q, and of the entries that p has more of
+    uint32_t near = 0;  // a bit to an entry
+#pragma unroll
+    for (int q = 0; q < E; ++q) {
+        const double ep = e.exp((double)x[q], c.mp, p.by);
+        s[0] += ep;
+        if (has_q) {
+            const double eq = e.exp((double)y[q], c.mq, p.by), bar = c.r * eq;
+            s[1] += eq;
+            const bool aside = bar > 0.0 && fabs(ep - bar) <= kNear * bar;
+            near |= (uint32_t)aside << q;
+            if (ep > bar && !aside) s[2] += ep, s[3] += eq;
+        }
+        // (all of them at once would not fit the registers)
+        if (q % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    // (rare: a few entries of a row)
+    int all_near = 0;
+    if (__syncthreads_or(near != 0)) {
+        const uint32_t mine = __popc(near), upto = wave_incl_scan_u32(mine);
+        if (lane_id() == kWave - 1) counts[wave_in_block()] = (int)upto;
+        __syncthreads();
+        int at = (int)(upto - mine);
+        for (int w = 0; w < kBlock / kWave; ++w) {
+            if (w < wave_in_block()) at += counts[w];
+            all_near += counts[w];
+        }
+        if (all_near > kAside) {
+            all_near = kAgain;
+        } else {
+#pragma unroll
+            for (int q = 0; q < E; ++q)
+                if (near >> q & 1)
+                    p.aside[(i * p.chunks + k) * kAside + at++] = double2{
+                        e.exp((double)x[q], c.mp, p.by), e.exp((double)y[q], c.mq, p.by)};
+        }
+    }
+    // without a draft's row only the refused token's chunk has anything aside
+    if (!p.draft && c.x >= k * kChunk && c.x < (k + 1) * kChunk) all_near = kAgain;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) s[n] = wave_sum_f64(s[n]);
+    if (lane_id() == 0)
+        for (int n = 0; n < 4; ++n) sums[wave_in_block()][n] = s[n];
     __syncthreads();
     if (threadIdx.x == 0) {
-        double2 t = s[0];
-        for (int w = 1; w < kBlock / kWave; ++w) t.x += s[w].x, t.y += s[w].y;
-        p.mass[i * p.chunks + k] = t;
+        double t[4];
+        for (int n = 0; n < 4; ++n)
+            t[n] = (sums[0][n] + sums[1][n]) + (sums[2][n] + sums[3][n]);
+        p.chunk[i * p.chunks + k] = Chunk{c.mp, t[0], t[1], t[2], t[3], all_near, 0};
     }
 }
+
+// ----------------------------------------------------------------------------
+// step 3
 
 // The sum over the threads below this one, and over all.
 __device__ __forceinline__ double block_before_f64(double v, double *all) {
@@ -290,81 +442,157 @@ __device__ __forceinline__ double block_before_f64(double v, double *all) {
     *all = sum;
     return base + before;
 }
-__device__ __forceinline__ int64_t block_min_i64(int64_t v) {
-    __shared__ int64_t s[kBlock / kWave];
+// The smallest of the threads' a and the largest of their b, in every thread.
+__device__ __forceinline__ void block_ends_i64(int64_t &a, int64_t &b) {
+    __shared__ int64_t s[2][kBlock / kWave];
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = min(v, (int64_t)__shfl_xor((long long)v, o));
-    if (lane_id() == 0) s[wave_in_block()] = v;
+    for (int o = 32; o >= 1; o >>= 1) {
+        a = min(a, (int64_t)__shfl_xor((long long)a, o));
+        b = max(b, (int64_t)__shfl_xor((long long)b, o));
+    }
+    if (lane_id() == 0) s[0][wave_in_block()] = a, s[1][wave_in_block()] = b;
     __syncthreads();
-    v = min(min(s[0], s[1]), min(s[2], s[3]));
+    a = min(min(s[0][0], s[0][1]), min(s[0][2], s[0][3]));
+    b = max(max(s[1][0], s[1][1]), max(s[1][2], s[1][3]));
     __syncthreads();
-    return v;
 }
-static_assert(kBlock == 4 * kWave, "four waves");
 
-template <int DT>
+// A thread's E weights from e0 on: of what the refused token leaves, or of p.
+template <int DT, int E>
+__device__ __forceinline__ void weights(const Verify &p, const Choice &c, int64_t i, int64_t e0, double m,
+                                        double r, bool residual, const Powers &e, double *w) {
+    float x[E], y[E];
+    load_each<DT, E>(p, c, i, e0, x, y);
+#pragma unroll
+    for (int q = 0; q < E; ++q) {
+        w[q] = e.exp((double)x[q], m, p.by);
+        if (!residual) continue;
+        if (p.draft)
+            w[q] = fmax(w[q] - r * e.exp((double)y[q], c.mq, p.by), 0.0);
+        else if (e0 + q == c.x)
+            w[q] = 0.0;
+    }
+}
+
+template <int DT, int E>
 __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
+    constexpr int kChunk = kBlock * E;
+    __shared__ Powers e;
+    __shared__ int todo, list[kBlock];
     const int64_t i = blockIdx.x;
     const Choice c = p.choice[i];
-    const double2 *mass = p.mass + i * p.chunks;
+    Chunk *chunk = p.chunk + i * p.chunks;
     const int t = threadIdx.x;
-    // the residual, unless it is 0 throughout; a stretch of chunks to a thread
     const int64_t each = (p.chunks + kBlock - 1) / kBlock, k0 = min(t * each, p.chunks),
                   k1 = min(k0 + each, p.chunks);
-    double all = 0.0, before = 0.0;
+    e.fill();
+    __syncthreads();
+    // the row's maximum, where chunks have their own
+    double m = c.mp;
+    if (p.k == 0) {
+        __shared__ double tops[kBlock / kWave];
+        m = -FLT_MAX;
+        for (int64_t k = k0; k < k1; ++k) m = fmax(m, chunk[k].m);
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
+        if (lane_id() == 0) tops[wave_in_block()] = m;
+        __syncthreads();
+        m = fmax(fmax(tops[0], tops[1]), fmax(tops[2], tops[3]));
+    }
+    auto mass_p = [&](int64_t k) {
+        return p.k == 0 ? chunk[k].sp * e.exp(chunk[k].m, m, p.by) : chunk[k].sp;
+    };
+    double sum = 0.0, sq = 0.0, all = 0.0;
+    for (int64_t k = k0; k < k1; ++k) sum += mass_p(k), sq += chunk[k].sq;
+    const double before_p = block_before_f64(sum, &all);
     bool residual = c.x >= 0;
+    double r = 0.0, before = before_p;
+    const double all_p = all;
+    if (residual) {
+        if (p.draft) {
+            sq = block_sum_f64(sq);
+            r = sq == 0.0 ? 0.0 : all_p / sq;
+            if (!(sq >= 0.0)) residual = false;  // the draft's row has no distribution
+        }
+    }
+    if (residual) {
+        // the chunks that step 2 left open, a turn of them at a time
+        for (int64_t a = 0; a < each; ++a) {
+            if (t == 0) todo = 0;
+            __syncthreads();
+            if (k0 + a < k1 && chunk[k0 + a].near == kAgain) list[atomicAdd(&todo, 1)] = t;
+            __syncthreads();
+            for (int n = 0; n < todo; ++n) {
+                const int64_t k = list[n] * each + a;
+                double w[E], s = 0.0;
+                weights<DT, E>(p, c, i, k * kChunk + t * E, m, r, true, e, w);
+#pragma unroll
+                for (int q = 0; q < E; ++q) s += w[q];
+                s = block_sum_f64(s);
+                if (t == 0) chunk[k].a = s;
+            }
+            __syncthreads();
+        }
+    }
+    auto mass = [&](int64_t k) -> double {
+        if (!residual) return mass_p(k);
+        const Chunk h = chunk[k];
+        if (h.near == kAgain) return h.a;
+        double w = p.draft ? fmax(h.a - r * h.b, 0.0) : h.sp;
+        for (int n = 0; n < h.near; ++n) {
+            const double2 z = p.aside[(i * p.chunks + k) * kAside + n];
+            w += fmax(z.x - r * z.y, 0.0);
+        }
+        return w;
+    };
     if (residual) {
         double s = 0.0;
-        for (int64_t k = k0; k < k1; ++k) s += mass[k].x;
+        for (int64_t k = k0; k < k1; ++k) s += mass(k);
         before = block_before_f64(s, &all);
-        residual = all > 0.0;
-    }
-    if (!residual) {
-        double s = 0.0;
-        for (int64_t k = k0; k < k1; ++k) s += mass[k].y;
-        before = block_before_f64(s, &all);
+        if (!(all > 0.0)) {
+            residual = false;
+            before = before_p;
+            all = all_p;
+        }
     }
     const double bar = (double)p.u[i * (p.k + 1) + p.k] * all;
     constexpr int64_t kNone = INT64_MAX;
     int64_t found = kNone, last = -1;
     double run = before, base = before;
     for (int64_t k = k0; k < k1; ++k) {
-        const double m = residual ? mass[k].x : mass[k].y;
-        if (found == kNone && m > 0.0 && run + m > bar) found = k, base = run;
-        run += m;
-        if (m > 0.0) last = k;
+        const double w = mass(k);
+        if (found == kNone && w > 0.0 && run + w > bar) found = k, base = run;
+        run += w;
+        if (w > 0.0) last = k;
     }
-    const int64_t chunk_found = block_min_i64(found);
-    const int64_t chunk_last = -block_min_i64(-last);
+    int64_t chunk_found = found, chunk_last = last;
+    block_ends_i64(chunk_found, chunk_last);
     __shared__ double s_base;
     if (found == chunk_found && found != kNone) s_base = base;
     __syncthreads();
     int64_t next = -1;
-    if (chunk_last >= 0) {
+    if (chunk_last >= 0 && all_p >= 0.0) {  // (not of a row with a NaN)
         // a sum that none exceeds: the last weight above 0
         const int64_t k = chunk_found != kNone ? chunk_found : chunk_last;
         const double limit = chunk_found != kNone ? bar : __builtin_inf();
-        double wp[kEach], wr[kEach], s = 0.0, sum;
-        const int64_t e0 = k * kChunk + t * kEach;
-        weights<DT>(p, c, i, e0, wp, wr);
+        double w[E], s = 0.0, total;
+        const int64_t e0 = k * kChunk + t * E;
+        weights<DT, E>(p, c, i, e0, m, r, residual, e, w);
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-            if (residual) wp[q] = wr[q];
-            s += wp[q];
-        }
-        double sofar = (chunk_found != kNone ? s_base : 0.0) + block_before_f64(s, &sum);
+        for (int q = 0; q < E; ++q) s += w[q];
+        double sofar = (chunk_found != kNone ? s_base : 0.0) + block_before_f64(s, &total);
         int64_t hit = kNone, end = -1;
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-            sofar += wp[q];
+        for (int q = 0; q < E; ++q) {
+            sofar += w[q];
             // (the sums before two threads differ in their last bits from one thread's
             // own: an entry of weight 0 may seem to pass the bar)
-            if (hit == kNone && wp[q] > 0.0 && sofar > limit) hit = e0 + q;
-            if (wp[q] > 0.0) end = e0 + q;
+            if (hit == kNone && w[q] > 0.0 && sofar > limit) hit = e0 + q;
+            if (w[q] > 0.0) end = e0 + q;
         }
-        const int64_t a = block_min_i64(hit), z = -block_min_i64(-end);
+        block_ends_i64(hit, end);
         // the chunk's sum and its entries' may differ in their last bits
-        next = a != kNone ? a : z;
+        next = hit != kNone ? hit : end;
     }
     for (int j = t; j <= p.k; j += kBlock) {
         int32_t o = -1;
@@ -377,19 +605,25 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
     if (t == 0) p.accepted[i] = c.at;
 }
 
+// ----------------------------------------------------------------------------
+// host side
+
+// Step 1's blocks: enough for an even load, of a tile at least.
+constexpr int64_t kWantParts = 4096;
+
 struct Space {
-    Parts cut;
     int64_t rows, chunks;
-    size_t parts, choice, total;  // offsets in the workspace
+    size_t choice, chunk, aside, total;  // offsets in the workspace
 };
 Space space_of(int64_t b, int32_t k, int64_t v) {
     Space s;
-    // rows are cut only up to kWantBlocks parts in all
+    // (rows are cut up to kWantParts parts in all, and a row has one at least)
     s.rows = b * (2 * k + 1);
-    s.chunks = cdiv(std::max<int64_t>(v, 1), kChunk);
-    s.parts = (size_t)align_up(std::max(s.rows, kWantBlocks) * (int64_t)sizeof(Sum));
-    s.choice = s.parts + (size_t)align_up(b * (int64_t)sizeof(Choice));
-    s.total = s.choice + (size_t)align_up(b * s.chunks * (int64_t)sizeof(double2));
+    s.chunks = cdiv(std::max<int64_t>(v, 1), kBlock * each_of(k));
+    s.choice = (size_t)align_up((s.rows + kWantParts) * (int64_t)sizeof(Sum));
+    s.chunk = s.choice + (size_t)align_up(b * (int64_t)sizeof(Choice));
+    s.aside = s.chunk + (size_t)align_up(b * s.chunks * (int64_t)sizeof(Chunk));
+    s.total = s.aside + (k > 0 ? (size_t)(b * s.chunks * kAside * (int64_t)sizeof(double2)) : 0);
     return s;
 }
 
@@ -422,24 +656,49 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
     if (!u || !out || !accepted || !aligned_to(u, 4) || !aligned_to(out, 4) || !aligned_to(accepted, 4))
         return PDB_ERR_INVALID_ARG;
     const Space sp = space_of(b, k, v);
-    if (!ws || ws_bytes < sp.total) return PDB_ERR_WORKSPACE;
+    if (!ws || !aligned_to(ws, 8) || ws_bytes < sp.total) return PDB_ERR_WORKSPACE;
     if (b * sp.chunks > INT32_MAX) return PDB_ERR_UNSUPPORTED;
     Verify p = {};
     p.target = target, p.draft = k > 0 ? draft : nullptr, p.tokens = tokens, p.ldt = ldt, p.ldq = ldq;
     p.v = v, p.b = (int32_t)b, p.k = k, p.index = index, p.u = u, p.inv_t = 1.0 / (double)temp;
+    p.by = p.inv_t * 0x1.71547652b82fep+6;
+    p.c = kLog2e / temp;
     p.out = out, p.accepted = accepted, p.status = status, p.chunks = sp.chunks;
     char *at = static_cast<char *>(ws);
     p.part = reinterpret_cast<Sum *>(at);
-    p.choice = reinterpret_cast<Choice *>(at + sp.parts);
-    p.mass = reinterpret_cast<double2 *>(at + sp.choice);
+    p.choice = reinterpret_cast<Choice *>(at + sp.choice);
+    p.chunk = reinterpret_cast<Chunk *>(at + sp.chunk);
+    p.aside = reinterpret_cast<double2 *>(at + sp.aside);
     return with_dtype(dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value;
-        const int64_t rows = b * (k + 1) + (p.draft ? b * k : 0);
-        p.cut = cut_rows(rows, v, Elem<DT>::kVec, kMostParts);
-        if (rows * p.cut.parts > INT32_MAX) return PDB_ERR_UNSUPPORTED;
-        k_verify_sums<DT><<<(unsigned)(rows * p.cut.parts), kBlock, 0, stream>>>(p);
-        k_verify_mass<DT><<<(unsigned)(b * p.chunks), kBlock, 0, stream>>>(p);
-        k_verify_pick<DT><<<(unsigned)b, kBlock, 0, stream>>>(p);
+        if (k > 0) {
+            const int64_t rows = b * (k + 1) + (p.draft ? b * k : 0);
+            const int64_t tile = kTileVecs * kBlock, tiles = std::max<int64_t>(cdiv(v / Elem<DT>::kVec, tile), 1);
+            const int64_t parts = std::min(std::min(kWantParts / rows, tiles), kMostParts);
+            const int64_t of_part = cdiv(tiles, std::max<int64_t>(parts, 1));
+            p.parts = (int32_t)cdiv(tiles, of_part);
+            p.vecs = (int32_t)std::min<int64_t>(of_part * tile, INT32_MAX / 2);
+            if (rows * p.parts > INT32_MAX) return PDB_ERR_UNSUPPORTED;
+            k_verify_sums<DT><<<(unsigned)(rows * p.parts), kBlock, 0, stream>>>(p);
+        }
+        // Where a sequence stops is found by each block of its chunks while they are few,
+        // which saves a launch (575 of them: 28 us against 30), else once (2,048: 58
+        // against 60; 4,096: 75 against 84).
+        const unsigned blocks = (unsigned)(b * p.chunks), rows = (unsigned)b;
+        if (k == 0) {
+            constexpr int E = each_of(0);
+            k_verify_chunks<DT, E, true><<<blocks, kBlock, 0, stream>>>(p);
+            k_verify_pick<DT, E><<<rows, kBlock, 0, stream>>>(p);
+        } else {
+            constexpr int E = each_of(1);
+            if (blocks <= 1024) {
+                k_verify_chunks<DT, E, true><<<blocks, kBlock, 0, stream>>>(p);
+            } else {
+                k_verify_choose<DT><<<rows, kBlock, 0, stream>>>(p);
+                k_verify_chunks<DT, E, false><<<blocks, kBlock, 0, stream>>>(p);
+            }
+            k_verify_pick<DT, E><<<rows, kBlock, 0, stream>>>(p);
+        }
         PDB_LAUNCHED();
         return PDB_OK;
     });

@@ -166,3 +166,77 @@ def test_near_borders(gpu):
     u = np.minimum(u, np.float32(1 - 2 ** -24))
     same(gpu, t, t64.reshape(n, 1, v), None, None, np.zeros((n, 0), np.int64),
          torch.from_numpy(u[:, None]).to(gpu))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("model", [True, False])
+def test_near_the_bar(gpu, dtype, model):
+    """Random numbers next to p / q, where 32-bit sums cannot tell: at every position of
+    a draft, those before it accepted."""
+    import torch
+
+    rng = np.random.default_rng(7)
+    b, k, v = 60, 4, 3001
+    t, t64, q, q64, x, u = draw_case(gpu, rng, b, k, v, dtype)
+    un = np.full((b, k + 1), 0.0, np.float32)
+    un[:, k] = rng.random(b)
+    for i in range(b):
+        j = i % k
+        p = ref.softmax(t64[i, j], 1.0)
+        w = ref.softmax(q64[i, j], 1.0) if model else np.ones(v)
+        x[i, j] = np.nonzero((p < w) & (p > 0))[0][i % 5]
+        bar = np.float32(p[x[i, j]] / w[x[i, j]])
+        un[i, j] = (bar, np.nextafter(bar, np.float32(0)), np.nextafter(bar, np.float32(1)))[i % 3]
+    r, _ = same(gpu, t, t64, q if model else None, q64, x, torch.from_numpy(un).to(gpu))
+    at = np.arange(b) % k
+    stopped = r.accepted.cpu().numpy() == at
+    assert stopped.any() and not stopped.all()   # both sides of the bar
+
+
+def test_residual_of_nearly_equal_rows(gpu):
+    """The draft has the target's logits but for the token that it proposes: what is left
+    of every other entry is a part in 1e5 of it, and its sign hangs on the exact sums."""
+    import torch
+
+    rng = np.random.default_rng(8)
+    b, k, v = 24, 1, 20_011
+    t, t64 = on_gpu(rng.normal(size=(b * 2, v)), "f32", gpu)
+    t64 = t64.reshape(b, 2, v)
+    q = t.view(b, 2, v)[:, 0].clone()
+    x = rng.integers(0, v, (b, 1))
+    for i in range(b):
+        p = ref.softmax(t64[i, 0], 1.0)
+        x[i, 0] = np.argmin(np.abs(p - 1e-5))
+        q[i, x[i, 0]] += 0.7
+    u = torch.from_numpy(rng.random((b, 2)).astype(np.float32)).to(gpu)
+    u[:, 0] = 0.9
+    r, _ = same(gpu, t, t64, q, f64(q).reshape(b, 1, v), x, u)
+    assert not r.accepted.any()
+
+
+def test_captured_and_replayed(gpu):
+    """Recorded into a graph, replayed on other inputs, with eager work between."""
+    import torch
+
+    native = native_mod()
+    rng = np.random.default_rng(9)
+    cases = [draw_case(gpu, rng, 6, 3, 9001, "bf16") for _ in range(3)]
+    t, _, q, _, x, u = (c.clone() if hasattr(c, "clone") else c for c in cases[0])
+    tok = torch.from_numpy(x).to(gpu)
+    native.pdb_draft_verify(t, u, tokens=tok, draft=q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = native.pdb_draft_verify(t, u, tokens=tok, draft=q)
+        one = native.pdb_draft_verify(t, u.view(-1, 1))
+    for c in cases + cases:
+        t.copy_(c[0])
+        q.copy_(c[2])
+        tok.copy_(torch.from_numpy(c[4]))
+        u.copy_(c[5])
+        graph.replay()
+        torch.cuda.synchronize()
+        out, acc = ref.verify(c[1], c[3], c[4], f64(c[5]), 1.0)
+        assert np.array_equal(r.tokens.cpu().numpy(), out) and np.array_equal(r.accepted.cpu().numpy(), acc)
+        eager = native.pdb_draft_verify(t, u.view(-1, 1))
+        assert torch.equal(one.tokens, eager.tokens)
