@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -596,6 +597,7 @@ def pdb_mb_barrier(rounds: int, blocks: int, device, ws=None, stream=None, opt=N
 
 _DTYPES = {torch.float32: PDB_F32, torch.float16: PDB_F16, torch.bfloat16: PDB_BF16}
 _INDEXES = {torch.int32: PDB_I32, torch.int64: PDB_I64}
+_DTYPE_OF, _SHAPE_OF = operator.attrgetter("dtype"), operator.attrgetter("shape")
 
 
 def _matrix(t, name, device=None):
@@ -1032,31 +1034,46 @@ def pdb_grad_workspace_bytes() -> int:
     return out.value
 
 
-def _tensors(ts, name, device, flat):
-    """Array of pdb_tensor of the tensors, as one row each where `flat`."""
+@functools.lru_cache(maxsize=64)
+def _one_row(n, kind):
+    """n pdb_tensor of one row and that type, without addresses and columns."""
+    return array.array("q", (0, 1, 0, 0, kind)) * n
+
+
+def _tensors(ts, name, device, like=None):
+    """(array of pdb_tensor, whether any has gaps) of tensors without gaps, as one row
+    each, or of matrices with unit column stride.  like: another such array, whose rows
+    and columns these tensors, without gaps, are to have."""
     n = len(ts)
+    types = list(map(_DTYPE_OF, ts))
     try:
-        kind = [_DTYPES[t.dtype] for t in ts]
+        kinds = [_DTYPES[types[0]]] if types.count(types[0]) == n else [_DTYPES[t] for t in types]
     except KeyError:
         raise TypeError("%s must be float32, float16 or bfloat16" % name) from None
-    if set(map(torch.Tensor.get_device, ts)) - {device} or device < 0:
+    if device < 0 or list(map(torch.Tensor.get_device, ts)).count(device) != n:
         raise ValueError("%s must be on one device" % name)
-    a = array.array("q", bytes(40 * n))
+    whole = list(map(torch.Tensor.is_contiguous, ts))
+    a = _one_row(n, kinds[0])[:]
     a[0::5] = array.array("q", map(torch.Tensor.data_ptr, ts))
-    a[4::5] = array.array("q", kind)
-    if flat:
-        size = array.array("q", map(torch.Tensor.numel, ts))
-        a[1::5], a[2::5], a[3::5] = array.array("q", [1]) * n, size, size
-        return a
-    for i, t in enumerate(ts):
-        if t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1):
-            a[5 * i + 1], a[5 * i + 2] = t.shape
-            a[5 * i + 3] = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-        elif t.is_contiguous():
-            a[5 * i + 1], a[5 * i + 2], a[5 * i + 3] = 1, t.numel(), t.numel()
+    if len(kinds) > 1:
+        a[4::5] = array.array("q", kinds)
+    if False not in whole:
+        if like is None:
+            a[2::5] = array.array("q", map(torch.Tensor.numel, ts))
+        else:
+            a[1::5], a[2::5], a[3::5] = like[1::5], like[2::5], like[2::5]
+        return a, False
+    for i, (size, step) in enumerate(zip(map(_SHAPE_OF, ts), map(torch.Tensor.stride, ts))):
+        if len(size) == 2 and (step[1] == 1 or size[1] <= 1):
+            rows, cols = size
+            a[5 * i + 1] = rows
+            a[5 * i + 2] = cols
+            a[5 * i + 3] = step[0] if rows > 1 else cols
+        elif whole[i]:
+            a[5 * i + 2] = ts[i].numel()
         else:
             raise ValueError("%s must be contiguous, or matrices with unit column stride" % name)
-    return a
+    return a, True
 
 
 def _grads(grads):
@@ -1069,7 +1086,7 @@ def _grads(grads):
 def pdb_grad_norm(grads, scale: float = 1.0, ws=None, stream=None) -> torch.Tensor:
     """|scale| times the norm of all the tensors together, a tensor of no dimension."""
     grads, dev = _grads(grads)
-    g = _tensors(grads, "grads", dev, all(map(torch.Tensor.is_contiguous, grads)))
+    g, _ = _tensors(grads, "grads", dev)
     norm = _empty(grads[0], (), torch.float32, stream)
     wp, size, ws = _space(ws, pdb_grad_workspace_bytes(), grads[0], stream)
     _check(load().pdb_grad_norm(g.buffer_info()[0], len(grads), scale, norm.data_ptr(), wp, size,
@@ -1086,11 +1103,13 @@ def pdb_grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, step: fl
     written where that is not finite."""
     grads, dev = _grads(grads)
     out = grads if out is None else list(out)
-    if len(out) != len(grads) or any(a.shape != b.shape for a, b in zip(grads, out)):
+    if out is not grads and list(map(_SHAPE_OF, out)) != list(map(_SHAPE_OF, grads)):
         raise ValueError("out must hold a tensor of the same shape for every gradient")
-    flat = all(map(torch.Tensor.is_contiguous, grads)) and all(map(torch.Tensor.is_contiguous, out))
-    g = _tensors(grads, "grads", dev, flat)
-    o = _tensors(out, "out", dev, flat)
+    g = o = _tensors(grads, "grads", dev)[0]
+    if out is not grads:
+        o, apart = _tensors(out, "out", dev, g)
+        if apart:  # rows further apart than their columns: the gradients by rows, too
+            g, _ = _tensors(grads, "grads", dev, o)
     norm = _empty(grads[0], (), torch.float32, stream)
     wp, size, ws = _space(ws, pdb_grad_workspace_bytes(), grads[0], stream)
     _check(load().pdb_grad_clip(g.buffer_info()[0], len(grads), scale, max_norm, step,

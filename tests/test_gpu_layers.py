@@ -377,3 +377,125 @@ def test_large_tensor(gpu):
     assert abs(float(native.pdb_grad_norm([g])) / want - 1) < 2 ** -23
     native.pdb_grad_clip([g], float(want) / 2)
     assert bool((g[:-3] == 0.5).all()) and bool((g[-3:] == 128).all())
+
+
+def test_layouts_that_differ(gpu):
+    """Gradients in rows further apart, outputs without gaps, and the other way round;
+    tensors of other dimensions among them."""
+    import torch
+
+    native = native_mod()
+    rng = np.random.default_rng(5)
+    shapes = [(40, 9), (7,), (2, 3, 4), (1, 300), (300, 1), (), (90, 130)]
+    for pads in ((4, 0), (0, 4), (4, 2), (0, 0)):
+        g = draw_grads(gpu, rng, shapes, ["bf16", "f32"], pads[0])
+        o = draw_grads(gpu, rng, shapes, ["f32"], pads[1])
+        want, bound, res, bounds = ref.clip([f64(t) for t in g], [f64(t) for t in o], 1.0, 2.0, -0.1, True)
+        norm = native.pdb_grad_clip(g, 2.0, out=o, step=-0.1, accumulate=True)
+        assert abs(float(norm) - want) <= bound
+        for i, t in enumerate(o):
+            check(f64(t), res[i], bounds[i], (pads, i))
+    with pytest.raises(ValueError):
+        native.pdb_grad_norm([torch.zeros(4, 6, device=gpu).t()])
+    with pytest.raises(ValueError):
+        native.pdb_grad_norm([torch.zeros(8, device=gpu)[::2]])
+    with pytest.raises(ValueError):
+        native.pdb_grad_norm([torch.zeros(8, device=gpu), torch.zeros(8)])
+    with pytest.raises(TypeError):
+        native.pdb_grad_norm([torch.zeros(8, device=gpu), torch.zeros(8, device=gpu).double()])
+    with pytest.raises(ValueError):
+        native.pdb_grad_clip([torch.zeros(4, 6, device=gpu)], 1.0, out=[torch.zeros(6, 4, device=gpu)])
+
+
+def test_captured_layers(gpu):
+    """The layer operators recorded into one graph and replayed on other values, with eager
+    work between the replays: the bits of the eager calls."""
+    import torch
+
+    native = native_mod()
+    n, d = 3000, 72
+    starts = torch.tensor([0, 700, 700, 1999, 3000], dtype=torch.int32, device=gpu)
+    x, g, dy = (t.to(torch.bfloat16) for t in torch.randn(3, n, d, device=gpu))
+    h0 = torch.randn(4, d, device=gpu)
+    w = [torch.randn(500, 33, device=gpu), torch.randn(d, device=gpu)]
+
+    def calls(w):
+        f = native.pdb_gated_scan(x, g, starts=starts, h0=h0, marks=True)
+        r = native.pdb_gated_scan_grad(dy, x, g, f.marks, starts=starts, h0=h0)
+        norm = native.pdb_grad_clip([r.dx, r.dgate, r.dh0], 0.5)
+        second = native.pdb_grad_clip([t * 2 for t in w], 1.0, out=w, step=-0.1, accumulate=True)
+        return [f.y, f.state, f.marks, r.dx, r.dgate, r.dh0, norm, second]
+
+    calls([t.clone() for t in w])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = calls(w)
+    for k in range(5):
+        with torch.no_grad():
+            for t in (x, g, dy):
+                t.copy_(torch.randn(n, d, device=gpu))
+            h0.copy_(torch.randn(4, d, device=gpu))
+        eager = [t.clone() for t in w]
+        want = calls(eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        assert all(torch.equal(a, b) for a, b in zip(w, eager))
+
+
+def test_memory_and_streams_of_layers(gpu):
+    """On a stream of its own, while the current one still reads blocks that it has freed."""
+    import torch
+
+    native = native_mod()
+    n, d = 4000, 136
+    x, g, dy = torch.randn(3, n, d, device=gpu)
+    big = torch.randn(4096, 4096, device=gpu)
+
+    def calls(stream):
+        f = native.pdb_gated_scan(x, g, batch=5, marks=True, stream=stream)
+        r = native.pdb_gated_scan_grad(dy, x, g, f.marks, batch=5, stream=stream)
+        return [f.y, f.state, f.marks, r.dx, r.dgate, native.pdb_grad_norm([x, g], stream=stream),
+                native.pdb_draft_verify(x, dy[:, :1].contiguous().sigmoid(), stream=stream).tokens]
+
+    want = [t.clone() for t in calls(None)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    sizes = [4 * n * d, 4 * 5 * d, 4 * d * 63, 4, 4 * n, native.pdb_gated_scan_workspace_bytes(n, d),
+             native.pdb_grad_workspace_bytes(), native.pdb_draft_verify_workspace_bytes(n, 0, d)]
+    for _ in range(3):
+        blocks = [torch.full((s,), 7, dtype=torch.uint8, device=gpu) for s in sizes for _ in range(3)]
+        torch.cuda.synchronize()
+        for _ in range(8):
+            big @ big
+        seen = [t.clone() for t in blocks]
+        del blocks
+        side.wait_stream(torch.cuda.current_stream())
+        got = calls(side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(bool((t == 7).all()) for t in seen)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_two_scans_at_once(gpu):
+    """Two chains of tiles on two streams, each in a workspace of its own."""
+    import torch
+
+    native = native_mod()
+    n, d = 60_000, 520
+    x, g = (t.to(torch.bfloat16) for t in torch.randn(2, n, d, device=gpu))
+    want = native.pdb_gated_scan(x, g, marks=True)
+    back = native.pdb_gated_scan_grad(x, x, g, want.marks)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a = native.pdb_gated_scan(x, g, marks=True, stream=streams[0])
+        b = native.pdb_gated_scan_grad(x, x, g, want.marks, stream=streams[1])
+        c = native.pdb_gated_scan(x, g, stream=streams[2])
+        torch.cuda.synchronize()
+        assert torch.equal(a.y, want.y) and torch.equal(c.y, want.y) and torch.equal(a.marks, want.marks)
+        assert torch.equal(b.dx, back.dx) and torch.equal(b.dgate, back.dgate)
