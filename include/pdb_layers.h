@@ -45,8 +45,8 @@ int pdb_gated_scan_workspace_bytes(int64_t n, int64_t d, size_t *bytes);
  * row is of no sequence).
  * A value that is not finite makes its channel not finite from its row to its
  * sequence's end, and reaches no other sequence.
- * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8,
- * for this call alone until it has run (tiles of rows pass their states through it; a
+ * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8
+ * (NULL in the decoding step: n = b, no starts), for this call alone until it has run (tiles of rows pass their states through it; a
  * wait of 2 s there, which only a workspace that something else writes brings about,
  * ends with NaN and *status = PDB_ERR_DEVICE). */
 int pdb_gated_scan(const void *x, int64_t ldx, const void *gate, int64_t ldg, int dtype, int64_t n,

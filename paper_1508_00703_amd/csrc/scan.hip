@@ -835,11 +835,13 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
         PDB_LAUNCHED();
         return PDB_OK;
     }
-    if (!ws || !aligned_to(ws, 8) || ws_bytes < scan_ws_bytes(p.n, p.d)) return PDB_ERR_WORKSPACE;
+    const bool step = !GRAD && !p.starts && p.len == 1;
+    if (!step && (!ws || !aligned_to(ws, 8) || ws_bytes < scan_ws_bytes(p.n, p.d)))
+        return PDB_ERR_WORKSPACE;
     if (cut.tiles * cut.strips > INT32_MAX) return PDB_ERR_UNSUPPORTED;
     p.tiles = (int32_t)cut.tiles;
     p.strips = (int32_t)cut.strips;
-    if (cut.tiles > 1) {
+    if (cut.tiles > 1 && !step) {
         p.ticket = static_cast<uint32_t *>(ws);
         p.total = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + kAlign);
         p.leave = reinterpret_cast<uint32_t *>(p.total + cut.tiles * cut.slots);
@@ -850,7 +852,7 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
         auto go = [&](auto wide) -> int {
             constexpr bool W = decltype(wide)::value;
             const unsigned grid = (unsigned)(cut.tiles * cut.strips);
-            if (!GRAD && !p.starts && p.len == 1 && p.n > 0) {
+            if (step) {
                 const int64_t vecs = cdiv(p.d, Elem<DT>::kVec);
                 if (cdiv(p.n * vecs, kBlock) > INT32_MAX) return PDB_ERR_UNSUPPORTED;
                 k_scan_step<DT, W><<<(unsigned)cdiv(p.n * vecs, kBlock), kBlock, 0, stream>>>(p, vecs);

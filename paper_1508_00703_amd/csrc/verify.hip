@@ -12,10 +12,12 @@
 // 2. of the row at which each sequence stopped, chunk by chunk in binary64: the sums of
 //    e_p and e_q (exp of logits below the row's maximum), and those over the entries that
 //    p has more of, e_p > r e_q with r = S_p / S_q: by step 1's r, since their exact r is
-//    known only behind this step.  Entries within kNear of it are put aside.
-// 3. with S_p and S_q, a chunk's residual is A - r B and what the entries put aside leave
-//    (a chunk of many of them is done again); the chunk that the random number picks is
-//    run through entry by entry.
+//    known only behind this step.  Entries within kNear of it have sums of their own, and
+//    the range of their e_p / e_q is kept.  (They may be many: logits of 16 bits lie on a
+//    grid, and so does e_p / e_q.)
+// 3. with S_p and S_q, a chunk's residual is A - r B, and the same of the entries near r if
+//    r is below their range (a chunk with r inside it is done again); the chunk that the
+//    random number picks is run through entry by entry.
 // Without drafted tokens step 1 is left out: chunks have maxima of their own.
 #include "pdb_softmax.h"
 
@@ -113,9 +115,8 @@ struct Choice {
 struct Chunk {
     double m, sp, sq;  // m: what the powers of p are below
     double a, b;       // of the entries with e_p > r e_q: the sums of e_p and of e_q
-    int32_t near, pad;  // entries put aside; kAgain: the chunk is to be done again
+    double an, bn, lo, hi;  // of those near it the same, and the range of e_p / e_q
 };
-constexpr int kAside = 8, kAgain = -1;
 struct Verify {
     const void *target, *draft, *tokens;
     int64_t ldt, ldq, v;
@@ -129,7 +130,6 @@ struct Verify {
     Sum *part;       // [rows][parts]: the targets' rows, then the drafts'
     Choice *choice;  // [b]
     Chunk *chunk;    // [b][chunks]
-    double2 *aside;  // [b][chunks][kAside]: e_p and e_q of entries put aside
 };
 
 // How many tokens a sequence has, the same in every lane.
@@ -226,9 +226,17 @@ static_assert(kBlock == 4 * kWave, "four waves");
 // The exact sum of a row, by the block.
 template <int DT>
 __device__ double exact_sum(const Verify &p, const char *row, double m, const Powers &e) {
+    constexpr int V = Elem<DT>::kVec;
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < p.v; i += kBlock)
-        s += e.exp((double)load1<DT>(row, i), m, p.by);
+    const int64_t whole = p.v / V;
+    for (int64_t i = threadIdx.x; i < whole; i += kBlock) {
+        float x[V];
+        load_elems<DT, V>(row, i * V, x);
+#pragma unroll
+        for (int q = 0; q < V; ++q) s += e.exp((double)x[q], m, p.by);
+    }
+    const int64_t rest = whole * V + threadIdx.x;
+    if (rest < p.v) s += e.exp((double)load1<DT>(row, rest), m, p.by);
     return block_sum_f64(s);
 }
 
@@ -344,7 +352,7 @@ template <int DT, int E, bool FUSED>
 __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
     constexpr int kChunk = kBlock * E;
     __shared__ Powers e;
-    __shared__ int counts[kBlock / kWave];
+    __shared__ double nears[kBlock / kWave][4];
     __shared__ double sums[kBlock / kWave][4];
     __shared__ float tops[kBlock / kWave];
     const int64_t i = blockIdx.x / p.chunks, k = blockIdx.x - i * p.chunks;
@@ -372,7 +380,7 @@ __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
     if ((FUSED || p.k == 0) && k == 0 && threadIdx.x == 0) p.choice[i] = c;
     const bool has_q = c.x >= 0 && p.draft;
     double s[4] = {0.0, 0.0, 0.0, 0.0};  // e_p, e_q, and of the entries that p has more of
-    uint32_t near = 0;  // a bit to an entry
+    double near[4] = {0.0, 0.0, __builtin_inf(), -__builtin_inf()};
 #pragma unroll
     for (int q = 0; q < E; ++q) {
         const double ep = e.exp((double)x[q], c.mp, p.by);
@@ -380,36 +388,29 @@ __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
         if (has_q) {
             const double eq = e.exp((double)y[q], c.mq, p.by), bar = c.r * eq;
             s[1] += eq;
-            const bool aside = bar > 0.0 && fabs(ep - bar) <= kNear * bar;
-            near |= (uint32_t)aside << q;
-            if (ep > bar && !aside) s[2] += ep, s[3] += eq;
+            if (bar > 0.0 && fabs(ep - bar) <= kNear * bar) {
+                const double ratio = ep / eq;
+                near[0] += ep, near[1] += eq;
+                near[2] = fmin(near[2], ratio), near[3] = fmax(near[3], ratio);
+            } else if (ep > bar) {
+                s[2] += ep, s[3] += eq;
+            }
         }
         // (all of them at once would not fit the registers)
         if (q % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
-    // (rare: a few entries of a row)
-    int all_near = 0;
-    if (__syncthreads_or(near != 0)) {
-        const uint32_t mine = __popc(near), upto = wave_incl_scan_u32(mine);
-        if (lane_id() == kWave - 1) counts[wave_in_block()] = (int)upto;
-        __syncthreads();
-        int at = (int)(upto - mine);
-        for (int w = 0; w < kBlock / kWave; ++w) {
-            if (w < wave_in_block()) at += counts[w];
-            all_near += counts[w];
-        }
-        if (all_near > kAside) {
-            all_near = kAgain;
-        } else {
+    const bool any = __syncthreads_or(near[3] >= 0.0);
+    if (any) {
 #pragma unroll
-            for (int q = 0; q < E; ++q)
-                if (near >> q & 1)
-                    p.aside[(i * p.chunks + k) * kAside + at++] = double2{
-                        e.exp((double)x[q], c.mp, p.by), e.exp((double)y[q], c.mq, p.by)};
+        for (int n = 0; n < 2; ++n) near[n] = wave_sum_f64(near[n]);
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            near[2] = fmin(near[2], __shfl_xor(near[2], o));
+            near[3] = fmax(near[3], __shfl_xor(near[3], o));
         }
+        if (lane_id() == 0)
+            for (int n = 0; n < 4; ++n) nears[wave_in_block()][n] = near[n];
     }
-    // without a draft's row only the refused token's chunk has anything aside
-    if (!p.draft && c.x >= k * kChunk && c.x < (k + 1) * kChunk) all_near = kAgain;
 #pragma unroll
     for (int n = 0; n < 4; ++n) s[n] = wave_sum_f64(s[n]);
     if (lane_id() == 0)
@@ -419,7 +420,13 @@ __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
         double t[4];
         for (int n = 0; n < 4; ++n)
             t[n] = (sums[0][n] + sums[1][n]) + (sums[2][n] + sums[3][n]);
-        p.chunk[i * p.chunks + k] = Chunk{c.mp, t[0], t[1], t[2], t[3], all_near, 0};
+        if (any) {
+            for (int n = 0; n < 2; ++n)
+                near[n] = (nears[0][n] + nears[1][n]) + (nears[2][n] + nears[3][n]);
+            near[2] = fmin(fmin(nears[0][2], nears[1][2]), fmin(nears[2][2], nears[3][2]));
+            near[3] = fmax(fmax(nears[0][3], nears[1][3]), fmax(nears[2][3], nears[3][3]));
+        }
+        p.chunk[i * p.chunks + k] = Chunk{c.mp, t[0], t[1], t[2], t[3], near[0], near[1], near[2], near[3]};
     }
 }
 
@@ -515,12 +522,17 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
             if (!(sq >= 0.0)) residual = false;  // the draft's row has no distribution
         }
     }
+    auto again = [&](int64_t k) {
+        return p.draft ? chunk[k].lo < r && r < chunk[k].hi
+                       : c.x >= k * kChunk && c.x < (k + 1) * kChunk;
+    };
     if (residual) {
-        // the chunks that step 2 left open, a turn of them at a time
+        // the chunks that step 2 left open, and without q that of the token, a turn of them
+        // at a time
         for (int64_t a = 0; a < each; ++a) {
             if (t == 0) todo = 0;
             __syncthreads();
-            if (k0 + a < k1 && chunk[k0 + a].near == kAgain) list[atomicAdd(&todo, 1)] = t;
+            if (k0 + a < k1 && again(k0 + a)) list[atomicAdd(&todo, 1)] = t;
             __syncthreads();
             for (int n = 0; n < todo; ++n) {
                 const int64_t k = list[n] * each + a;
@@ -529,7 +541,7 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
 #pragma unroll
                 for (int q = 0; q < E; ++q) s += w[q];
                 s = block_sum_f64(s);
-                if (t == 0) chunk[k].a = s;
+                if (t == 0) chunk[k].m = s;  // (read for k = 0 only)
             }
             __syncthreads();
         }
@@ -537,13 +549,10 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
     auto mass = [&](int64_t k) -> double {
         if (!residual) return mass_p(k);
         const Chunk h = chunk[k];
-        if (h.near == kAgain) return h.a;
-        double w = p.draft ? fmax(h.a - r * h.b, 0.0) : h.sp;
-        for (int n = 0; n < h.near; ++n) {
-            const double2 z = p.aside[(i * p.chunks + k) * kAside + n];
-            w += fmax(z.x - r * z.y, 0.0);
-        }
-        return w;
+        if (again(k)) return h.m;
+        if (!p.draft) return h.sp;
+        const double near = r <= h.lo ? h.an - r * h.bn : 0.0;
+        return fmax(h.a - r * h.b, 0.0) + fmax(near, 0.0);
     };
     if (residual) {
         double s = 0.0;
@@ -613,7 +622,7 @@ constexpr int64_t kWantParts = 4096;
 
 struct Space {
     int64_t rows, chunks;
-    size_t choice, chunk, aside, total;  // offsets in the workspace
+    size_t choice, chunk, total;  // offsets in the workspace
 };
 Space space_of(int64_t b, int32_t k, int64_t v) {
     Space s;
@@ -622,8 +631,7 @@ Space space_of(int64_t b, int32_t k, int64_t v) {
     s.chunks = cdiv(std::max<int64_t>(v, 1), kBlock * each_of(k));
     s.choice = (size_t)align_up((s.rows + kWantParts) * (int64_t)sizeof(Sum));
     s.chunk = s.choice + (size_t)align_up(b * (int64_t)sizeof(Choice));
-    s.aside = s.chunk + (size_t)align_up(b * s.chunks * (int64_t)sizeof(Chunk));
-    s.total = s.aside + (k > 0 ? (size_t)(b * s.chunks * kAside * (int64_t)sizeof(double2)) : 0);
+    s.total = s.chunk + (size_t)align_up(b * s.chunks * (int64_t)sizeof(Chunk));
     return s;
 }
 
@@ -668,7 +676,6 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
     p.part = reinterpret_cast<Sum *>(at);
     p.choice = reinterpret_cast<Choice *>(at + sp.choice);
     p.chunk = reinterpret_cast<Chunk *>(at + sp.chunk);
-    p.aside = reinterpret_cast<double2 *>(at + sp.aside);
     return with_dtype(dtype, [&](auto dt) -> int {
         constexpr int DT = decltype(dt)::value;
         if (k > 0) {

@@ -988,13 +988,20 @@ def pdb_gated_scan(x: torch.Tensor, gate: torch.Tensor, starts=None, batch=None,
     f = torch.float32
     if out is None:
         out = _empty(x, x.shape, x.dtype, stream)
-    yp, ldy = _rows(out, "out", x, dev)
+        yp, ldy = out.data_ptr(), d
+    else:
+        yp, ldy = _rows(out, "out", x, dev)
     if state is None:
         state = _empty(x, (b, d), f, stream)
+        sto = state.data_ptr()
+    else:
+        sto = hp if state is h0 else _state(state, "state", b, d, dev)
     mk = _empty(x, (-(-n // PDB_SCAN_MARK), d), f, stream) if marks else None
-    wp, size, ws = _space(ws, pdb_gated_scan_workspace_bytes(n, d), x, stream)
-    _check(load().pdb_gated_scan(xp, ldx, gp, ldg, dt, n, d, sp, b, hp, yp, ldy,
-                                 _state(state, "state", b, d, dev),
+    if ws is None and starts is None and b == n:
+        wp, size = None, 0
+    else:
+        wp, size, ws = _space(ws, pdb_gated_scan_workspace_bytes(n, d), x, stream)
+    _check(load().pdb_gated_scan(xp, ldx, gp, ldg, dt, n, d, sp, b, hp, yp, ldy, sto,
                                  mk.data_ptr() if marks else None, _status(status, dev), wp, size,
                                  _raw_stream(stream, dev)), "pdb_gated_scan")
     return GatedScan(out, state, mk)
