@@ -163,9 +163,32 @@ __device__ __forceinline__ void find_edges(const Scan &p, int64_t r0, bool last_
         }
     } else {
         const int32_t *starts = p.starts;
-        lo = max((int64_t)starts[0], (int64_t)0);
-        hi = min((int64_t)starts[p.b], p.n);
-        for (int64_t j0 = first;; j0 += kWave) {
+        // The first few offsets by scalar loads, which do not wait behind the tile's rows.
+        // (Their order is not relied on: what lies outside the tile is left out.)
+        const auto *at_once = (const __attribute__((address_space(4))) int32_t *)starts;
+        constexpr int kFew = 4;
+        const int64_t j1 = __builtin_amdgcn_readfirstlane(first);
+        int64_t few[kFew + 2];  // offsets j1 - 1 .. j1 + kFew
+#pragma unroll
+        for (int i = 0; i < kFew + 2; ++i) {
+            const int64_t j = j1 - 1 + i;
+            few[i] = j < 0 ? INT64_MIN : j > p.b ? INT64_MAX : (int64_t)at_once[j];
+        }
+        lo = max((int64_t)at_once[0], (int64_t)0);
+        hi = min((int64_t)at_once[p.b], p.n);
+        bool done = false;
+#pragma unroll
+        for (int i = 1; i <= kFew; ++i) {
+            const int64_t j = j1 - 1 + i, at = few[i], next = few[i + 1], before = few[i - 1];
+            done |= j > p.b || at > r1;
+            // empty sequences have states to write: below
+            if (!done && j < p.b && next <= at) break;
+            if (!done && l == 0) {
+                if (j < p.b && at >= r0 && at < r1) e.begin[at - r0] = (int)j;
+                if (j > 0 && before < at && at > r0) e.end[at - 1 - r0] = (int)j - 1;
+            }
+        }
+        for (int64_t j0 = first; !done; j0 += kWave) {
             const int64_t j = j0 + l;
             const bool have = j <= p.b;
             const int64_t at = have ? starts[j] : INT64_MAX;
@@ -431,7 +454,7 @@ struct Fetched {
     static_assert(3 * kEach == kReach - 1, "thirds");
     unsigned long long map[kReach - 1][kStripLanes * V];
     float leave[kStripLanes * V];
-    int late;
+    int late, cut;  // a wait given up; a cut among the maps, so that no state is waited for
 };
 template <int V>
 __device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, int third, Fetched<V> &f) {
@@ -457,8 +480,14 @@ __device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, i
         }
         __builtin_amdgcn_s_sleep(1);
     }
+    bool cut = false;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) f.map[third * kEach + j][slot_of<V>()] = w[j];
+    for (int j = 0; j < kEach; ++j) {
+        f.map[third * kEach + j][slot_of<V>()] = w[j];
+        cut |= third * kEach + j < turn && is_cut(map_of(w[j]).a);
+    }
+    // (a tile with a sequence's beginning has cuts in all its slots)
+    if (__all(cut)) __hip_atomic_store(&f.cut, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
 // The block's own map, and the state behind the tile kReach before.
@@ -467,12 +496,15 @@ __device__ __forceinline__ void chain_wait(const Scan &p, int turn, int strip, M
     if (!p.ticket) return;
     const Link<V> l(p, turn, strip);
     if (turn < p.tiles - 1 && l.mine) post(p.total + l.at, word_of(m));
+    const bool cut = __all(is_cut(m.a));  // what leaves the tile does not hang on what enters
+    if (cut && turn + kReach < p.tiles && l.mine) post(p.leave + l.at, word_of(m.c));
     uint32_t h = 0;
     if (turn >= kReach) {
         const int64_t t0 = now_ticks();
         while (true) {
             h = peek(p.leave + (l.at - kReach * l.slots));
             if (!__any(h == ~0u)) break;
+            if (__hip_atomic_load(&f.cut, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)) break;
             if (__any(give_up(p, t0))) {
                 f.late = 1;
                 break;
@@ -497,7 +529,7 @@ __device__ __forceinline__ float chain_end(const Scan &p, int turn, int strip, M
         if (p.status) *p.status = PDB_ERR_DEVICE;
     }
     const Link<V> l(p, turn, strip);
-    if (first && turn + kReach < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
+    if (first && !is_cut(m.a) && turn + kReach < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
     return h;
 }
 
@@ -528,7 +560,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
         if (lane_id() == 0) {
             e.dealt = w;
             e.first = first;
-            fetched.late = 0;
+            fetched.late = fetched.cut = 0;
         }
     }
     __syncthreads();
@@ -638,7 +670,7 @@ __global__ __launch_bounds__(kBlock, 3) void k_scan_grad(Scan p) {
         if (lane_id() == 0) {
             e.dealt = w;
             e.first = first;
-            fetched.late = 0;
+            fetched.late = fetched.cut = 0;
         }
     }
     __syncthreads();
