@@ -201,15 +201,18 @@ __global__ __launch_bounds__(kBlock) void k_verify_sums(Verify p) {
 // ----------------------------------------------------------------------------
 // step 2
 
-// A row's maximum and sum from its parts', the same in every lane.
-__device__ __forceinline__ Sum join_sums(const Verify &p, int64_t row) {
-    Sum t = {-FLT_MAX, 0.0};
-    if (lane_id() < p.parts) t = p.part[row * p.parts + lane_id()];
-    double m = t.m;
+// Four sums over the wave: of s[n] in lane 16 n.  Halves, then quarters of the wave take a
+// share of the sums each: 7 exchanges instead of 24.
+__device__ __forceinline__ double wave_sums_f64(const double (&s)[4]) {
+    const bool up = lane_id() & 32, odd = lane_id() & 16;
+    double a = up ? s[2] : s[0], b = up ? s[3] : s[1];
+    a += __shfl_xor(up ? s[0] : s[2], 32);
+    b += __shfl_xor(up ? s[1] : s[3], 32);
+    double v = odd ? b : a;
+    v += __shfl_xor(odd ? a : b, 16);
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
-    raise(t, m, p.inv_t);
-    return {m, wave_sum_f64(t.s)};
+    for (int o = 8; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+    return v;
 }
 
 __device__ __forceinline__ double block_sum_f64(double v) {
@@ -247,13 +250,28 @@ __device__ __forceinline__ Choice choose(const Verify &p, int64_t i, const Power
     __shared__ unsigned long long stops, nears;
     const int have = drafted(p, i), wave = wave_in_block(), j = lane_id();
     const int64_t targets = (int64_t)p.b * (p.k + 1);
-    for (int r = wave; r <= have; r += kBlock / kWave) {
-        const Sum s = join_sums(p, i * (p.k + 1) + r);
-        if (lane_id() == 0) st[r] = s;
-        if (r < have && p.draft) {
-            const Sum d = join_sums(p, targets + i * p.k + r);
-            if (lane_id() == 0) sq[r] = d;
-        }
+    // what the decision looks at, asked for before the sums are joined
+    int32_t x = -1;
+    float z = 0.0f, y = 0.0f, u = 0.0f;
+    if (wave == 0 && j < have) {
+        x = read_token(p.tokens, p.index, i * p.k + j, p.v, nullptr);
+        u = p.u[i * (p.k + 1) + j];
+        z = load1<DT>(p.target, (i * (p.k + 1) + j) * p.ldt + x);
+        if (p.draft) y = load1<DT>(p.draft, (i * p.k + j) * p.ldq + x);
+    }
+    // a row's parts to a group of lanes: the targets' rows, then the drafts'
+    const int group = p.parts <= 8 ? 8 : kWave, of_wave = kWave / group, l = lane_id() & (group - 1);
+    const int rows = have + 1 + (p.draft ? have : 0);
+    for (int r0 = wave * of_wave; r0 < rows; r0 += of_wave * (kBlock / kWave)) {
+        const int r = r0 + lane_id() / group;
+        const int64_t row = r <= have ? i * (p.k + 1) + r : targets + i * p.k + (r - have - 1);
+        Sum t = {-FLT_MAX, 0.0};
+        if (r < rows && l < p.parts) t = p.part[row * p.parts + l];
+        double m = t.m;
+        for (int o = group / 2; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
+        raise(t, m, p.inv_t);
+        for (int o = group / 2; o >= 1; o >>= 1) t.s += __shfl_xor(t.s, o);
+        if (r < rows && l == 0) (r <= have ? st[r] : sq[r - have - 1]) = Sum{m, t.s};
     }
     __syncthreads();
     // a position to a lane of the first wave: whether it is refused, and whether step 1's
@@ -261,15 +279,10 @@ __device__ __forceinline__ Choice choose(const Verify &p, int64_t i, const Power
     auto decide = [&](bool exact) {
         bool stop = j >= have, near = false;
         if (!stop) {
-            const int32_t x = read_token(p.tokens, p.index, i * p.k + j, p.v, nullptr);
-            const float z = load1<DT>(p.target, (i * (p.k + 1) + j) * p.ldt + x);
             const double px = e.exp((double)z, st[j].m, p.by) / st[j].s;
             double qx = 1.0;
-            if (p.draft) {
-                const float y = load1<DT>(p.draft, (i * p.k + j) * p.ldq + x);
-                qx = sq[j].s == 0.0 ? 0.0 : e.exp((double)y, sq[j].m, p.by) / sq[j].s;
-            }
-            const double bar = (double)p.u[i * (p.k + 1) + j] * qx;
+            if (p.draft) qx = sq[j].s == 0.0 ? 0.0 : e.exp((double)y, sq[j].m, p.by) / sq[j].s;
+            const double bar = (double)u * qx;
             stop = !(bar < px);
             near = px > 0.0 && fabs(px - bar) <= kNear * px;
         }
@@ -356,19 +369,20 @@ __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
     __shared__ double sums[kBlock / kWave][4];
     __shared__ float tops[kBlock / kWave];
     const int64_t i = blockIdx.x / p.chunks, k = blockIdx.x - i * p.chunks;
-    const int64_t e0 = k * kChunk + threadIdx.x * E;
     e.fill();
     __syncthreads();
     Choice c = {0.0, 0.0, 0.0, 0, -1};
-    float x[E], y[E];
     if (p.k > 0) {
         if constexpr (FUSED)
             c = choose<DT>(p, i, e);
         else
             c = p.choice[i];
-        load_each<DT, E>(p, c, i, e0, x, y);
-    } else {
-        load_each<DT, E>(p, c, i, e0, x, y);
+    }
+    const bool has_q = c.x >= 0 && p.draft;
+    const int64_t e0 = k * kChunk + threadIdx.x * E;
+    float x[E], y[E];
+    load_each<DT, E>(p, c, i, e0, x, y);
+    if (p.k == 0) {
         float top = -FLT_MAX;
 #pragma unroll
         for (int q = 0; q < E; ++q) top = fmaxf(top, x[q]);
@@ -378,7 +392,6 @@ __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
         c.mp = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     }
     if ((FUSED || p.k == 0) && k == 0 && threadIdx.x == 0) p.choice[i] = c;
-    const bool has_q = c.x >= 0 && p.draft;
     double s[4] = {0.0, 0.0, 0.0, 0.0};  // e_p, e_q, and of the entries that p has more of
     double near[4] = {0.0, 0.0, __builtin_inf(), -__builtin_inf()};
 #pragma unroll
@@ -411,10 +424,13 @@ __global__ __launch_bounds__(kBlock) void k_verify_chunks(Verify p) {
         if (lane_id() == 0)
             for (int n = 0; n < 4; ++n) nears[wave_in_block()][n] = near[n];
     }
-#pragma unroll
-    for (int n = 0; n < 4; ++n) s[n] = wave_sum_f64(s[n]);
-    if (lane_id() == 0)
-        for (int n = 0; n < 4; ++n) sums[wave_in_block()][n] = s[n];
+    if (has_q) {
+        const double v = wave_sums_f64(s);
+        if (lane_id() % 16 == 0) sums[wave_in_block()][lane_id() / 16] = v;
+    } else {
+        s[0] = wave_sum_f64(s[0]);
+        if (lane_id() < 4) sums[wave_in_block()][lane_id()] = lane_id() == 0 ? s[0] : 0.0;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
         double t[4];
@@ -494,23 +510,27 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
                   k1 = min(k0 + each, p.chunks);
     e.fill();
     __syncthreads();
+    // (of up to kBlock chunks each thread keeps its own)
+    __shared__ double redone[kBlock];
+    const bool single = each == 1;
+    Chunk own = {};
+    if (single && k0 < k1) own = chunk[k0];
+    auto at = [&](int64_t k) { return single ? own : chunk[k]; };
     // the row's maximum, where chunks have their own
     double m = c.mp;
     if (p.k == 0) {
         __shared__ double tops[kBlock / kWave];
         m = -FLT_MAX;
-        for (int64_t k = k0; k < k1; ++k) m = fmax(m, chunk[k].m);
+        for (int64_t k = k0; k < k1; ++k) m = fmax(m, at(k).m);
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
         if (lane_id() == 0) tops[wave_in_block()] = m;
         __syncthreads();
         m = fmax(fmax(tops[0], tops[1]), fmax(tops[2], tops[3]));
     }
-    auto mass_p = [&](int64_t k) {
-        return p.k == 0 ? chunk[k].sp * e.exp(chunk[k].m, m, p.by) : chunk[k].sp;
-    };
+    auto mass_p = [&](const Chunk &h) { return p.k == 0 ? h.sp * e.exp(h.m, m, p.by) : h.sp; };
     double sum = 0.0, sq = 0.0, all = 0.0;
-    for (int64_t k = k0; k < k1; ++k) sum += mass_p(k), sq += chunk[k].sq;
+    for (int64_t k = k0; k < k1; ++k) sum += mass_p(at(k)), sq += at(k).sq;
     const double before_p = block_before_f64(sum, &all);
     bool residual = c.x >= 0;
     double r = 0.0, before = before_p;
@@ -523,8 +543,7 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
         }
     }
     auto again = [&](int64_t k) {
-        return p.draft ? chunk[k].lo < r && r < chunk[k].hi
-                       : c.x >= k * kChunk && c.x < (k + 1) * kChunk;
+        return p.draft ? at(k).lo < r && r < at(k).hi : c.x >= k * kChunk && c.x < (k + 1) * kChunk;
     };
     if (residual) {
         // the chunks that step 2 left open, and without q that of the token, a turn of them
@@ -541,15 +560,20 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
 #pragma unroll
                 for (int q = 0; q < E; ++q) s += w[q];
                 s = block_sum_f64(s);
-                if (t == 0) chunk[k].m = s;  // (read for k = 0 only)
+                if (t == 0) {
+                    if (single)
+                        redone[k] = s;
+                    else
+                        chunk[k].m = s;  // (read for k = 0 only)
+                }
             }
             __syncthreads();
         }
     }
     auto mass = [&](int64_t k) -> double {
-        if (!residual) return mass_p(k);
-        const Chunk h = chunk[k];
-        if (again(k)) return h.m;
+        const Chunk h = at(k);
+        if (!residual) return mass_p(h);
+        if (again(k)) return single ? redone[k] : h.m;
         if (!p.draft) return h.sp;
         const double near = r <= h.lo ? h.an - r * h.bn : 0.0;
         return fmax(h.a - r * h.b, 0.0) + fmax(near, 0.0);
@@ -688,6 +712,9 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
             if (rows * p.parts > INT32_MAX) return PDB_ERR_UNSUPPORTED;
             k_verify_sums<DT><<<(unsigned)(rows * p.parts), kBlock, 0, stream>>>(p);
         }
+        // Where a sequence stops is found by each block of its chunks while they are few,
+        // which saves a launch (575 of them: 28 us against 30), else once (2,048: 58
+        // against 60; 4,096: 75 against 84).
         // Where a sequence stops is found by each block of its chunks while they are few,
         // which saves a launch (575 of them: 28 us against 30), else once (2,048: 58
         // against 60; 4,096: 75 against 84).
