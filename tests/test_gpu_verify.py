@@ -240,3 +240,25 @@ def test_captured_and_replayed(gpu):
         assert np.array_equal(r.tokens.cpu().numpy(), out) and np.array_equal(r.accepted.cpu().numpy(), acc)
         eager = native.pdb_draft_verify(t, u.view(-1, 1))
         assert torch.equal(one.tokens, eager.tokens)
+
+
+@pytest.mark.parametrize("dtype,v", [("f32", 300_000), ("bf16", 700_001)])
+def test_rising_rows(gpu, dtype, v):
+    """Logits that rise along the row, so that the maximum is raised all the way: sums
+    next to the bar."""
+    import torch
+
+    rng = np.random.default_rng(10)
+    b, k = 3, 2
+    z = np.sort(rng.normal(size=(b * (k + 1), v)) * 2, axis=1)
+    t, t64 = on_gpu(z, dtype, gpu)
+    q, q64 = on_gpu(z[: b * k] * 0.9, dtype, gpu)
+    t64, q64 = t64.reshape(b, k + 1, v), q64.reshape(b, k, v)
+    x = np.zeros((b, k), np.int64)
+    u = rng.random((b, k + 1)).astype(np.float32)
+    for i in range(b):
+        p, w = ref.softmax(t64[i, 0], 1.0), ref.softmax(q64[i, 0], 1.0)
+        x[i, 0] = np.nonzero(p < w)[0][-1 - i]
+        x[i, 1] = v - 1 - i
+        u[i, 0] = np.nextafter(np.float32(p[x[i, 0]] / w[x[i, 0]]), np.float32(i % 2))
+    same(gpu, t, t64, q, q64, x, torch.from_numpy(u).to(gpu))
