@@ -27,8 +27,9 @@ namespace pdbk {
 namespace {
 
 // Consecutive entries of a thread: a chunk is kBlock times as many.  Drawing alone, without
-// drafted tokens, is bound by the exponentials (256 rows of 131,072: 43 us with 16, 54 with
-// 8); behind a draft it is latency (1 row of four: 22 us with 8, 24 with 16).
+// drafted tokens, is bound by the exponentials (256 rows of 131,072: 40 us with 16, 46 with
+// 8); behind a draft by latency and registers (1 sequence of four: 20 us with 8, 23 with 16;
+// 64 of five: 70 and 73).
 constexpr int each_of(int32_t k) { return k == 0 ? 16 : 8; }
 constexpr double kLowest = -700.0;  // powers below this count as 0
 // What step 1's sums may be off by, relatively, two rows of them.  In units of 2^-24: an
@@ -718,11 +719,8 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
             k_verify_sums<DT><<<(unsigned)(rows * p.parts), kBlock, 0, stream>>>(p);
         }
         // Where a sequence stops is found by each block of its chunks while they are few,
-        // which saves a launch (575 of them: 28 us against 30), else once (2,048: 58
-        // against 60; 4,096: 75 against 84).
-        // Where a sequence stops is found by each block of its chunks while they are few,
-        // which saves a launch (575 of them: 28 us against 30), else once (2,048: 58
-        // against 60; 4,096: 75 against 84).
+        // which saves a launch (64 of them: 20 us against 22, 575: 28 against 30), else once
+        // (2,048: 59 against 62; 4,096: 70 against 73).
         const unsigned blocks = (unsigned)(b * p.chunks), rows = (unsigned)b;
         if (k == 0) {
             constexpr int E = each_of(0);
