@@ -47,7 +47,7 @@ int pdb_gated_scan_workspace_bytes(int64_t n, int64_t d, size_t *bytes);
  * sequence's end, and reaches no other sequence.
  * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8
  * (NULL in the decoding step: n = b, no starts), for this call alone until it has run (tiles of rows pass their states through it; a
- * wait of 2 s there, which only a workspace that something else writes brings about,
+ * wait of 20 s there, which only a workspace that something else writes brings about,
  * ends with NaN and *status = PDB_ERR_DEVICE). */
 int pdb_gated_scan(const void *x, int64_t ldx, const void *gate, int64_t ldg, int dtype, int64_t n,
                    int64_t d, const int32_t *starts, int64_t b, const float *h0, void *y,
@@ -97,7 +97,7 @@ int pdb_grad_norm(const pdb_tensor *grads, int64_t count, float scale, float *no
  * or, with accumulate = 1, that added to what out_i holds (clipped gradient
  * descent: out the parameters, step = -lr).  outs: host array of `count` tensors,
  * each with its gradient's rows and columns, of any of the types; an out may be
- * its gradient (same pointer, type and row stride).  The factor is rounded to
+ * its gradient (same pointer, type and row stride), and no out may be another's.  The factor is rounded to
  * binary32 once, and the result to out's type.  max_norm >= 0 or +inf; step
  * finite.  Where norm[0] is not finite nothing is written but norm[0]; where the
  * factor is 1 an out that is its gradient is not written.  ws: at least

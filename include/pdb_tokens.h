@@ -168,7 +168,7 @@ int pdb_draft_verify_workspace_bytes(int64_t b, int32_t k, int64_t v, size_t *by
  * Rows of nothing but -inf, or with a NaN or +inf, have no distribution: as the
  * target's they refuse, and the next token is -1; as the draft's, those of -inf have
  * q = 0, the others refuse and leave p.  temp > 0 and finite.  0 <= k <=
- * PDB_MAX_DRAFT, v > 0, b (k + 1) < 2^31.  ws: at least
+ * PDB_MAX_DRAFT, v > 0, b (k + 1) and b v / 2048 < 2^31.  ws: at least
  * pdb_draft_verify_workspace_bytes(b, k, v). */
 int pdb_draft_verify(const void *target, int64_t ldt, const void *draft, int64_t ldq, int dtype,
                      int64_t b, int32_t k, int64_t v, const void *tokens, int index,

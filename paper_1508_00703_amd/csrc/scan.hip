@@ -408,7 +408,7 @@ __device__ __forceinline__ uint32_t deal(const Scan &p) {
 }
 
 constexpr int kReach = 16;  // tiles that a hop of the chain passes
-constexpr int64_t kPatience = 200000000;  // ticks of the 100 MHz clock: 2 s
+constexpr int64_t kPatience = 2000000000;  // ticks of the 100 MHz clock: 20 s
 constexpr int64_t kUneasy = 100000;       // 1 ms
 
 template <typename T>

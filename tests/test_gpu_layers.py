@@ -405,6 +405,10 @@ def test_layouts_that_differ(gpu):
         native.pdb_grad_norm([torch.zeros(8, device=gpu), torch.zeros(8, device=gpu).double()])
     with pytest.raises(ValueError):
         native.pdb_grad_clip([torch.zeros(4, 6, device=gpu)], 1.0, out=[torch.zeros(6, 4, device=gpu)])
+    w = torch.ones(4, 6, device=gpu)
+    with pytest.raises(ValueError, match="twice"):
+        native.pdb_grad_clip([w, w], 1.0)
+    assert abs(float(native.pdb_grad_norm([w, w])) / 48 ** 0.5 - 1) < 1e-6   # to read twice is no harm
 
 
 def test_captured_layers(gpu):

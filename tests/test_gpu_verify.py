@@ -262,3 +262,6 @@ def test_rising_rows(gpu, dtype, v):
         x[i, 1] = v - 1 - i
         u[i, 0] = np.nextafter(np.float32(p[x[i, 0]] / w[x[i, 0]]), np.float32(i % 2))
     same(gpu, t, t64, q, q64, x, torch.from_numpy(u).to(gpu))
+    same(gpu, t, t64, None, None, x, torch.from_numpy(u).to(gpu))
+    u[:, 0] = 0.99
+    same(gpu, t, t64, None, None, x, torch.from_numpy(u).to(gpu))
