@@ -157,7 +157,7 @@ int pdb_draft_verify_workspace_bytes(int64_t b, int32_t k, int64_t v, size_t *by
  *   exceeds u_k times their sum.
  * A token is drawn from p, too, where max(p_j - q_j, 0) is 0 throughout, and the last
  * index of weight > 0 where no running sum exceeds (u = 1).  Probabilities and sums
- * are binary64; logits more than 700 temp below their row's largest count as -inf.
+ * are binary64, and so is temp; logits more than 700 temp below their row's largest count as -inf.
  * target: device, b (k + 1) x v, row stride ldt: sequence i's rows i (k + 1) + j.
  * draft: device, b k x v, row stride ldq, of the same type: rows i k + j; or NULL for
  * tokens proposed without a distribution (q_j = 1 at x_j).  tokens: device, b x k of
@@ -172,7 +172,7 @@ int pdb_draft_verify_workspace_bytes(int64_t b, int32_t k, int64_t v, size_t *by
  * pdb_draft_verify_workspace_bytes(b, k, v). */
 int pdb_draft_verify(const void *target, int64_t ldt, const void *draft, int64_t ldq, int dtype,
                      int64_t b, int32_t k, int64_t v, const void *tokens, int index,
-                     const float *u, float temp, int32_t *out, int32_t *accepted, int32_t *status,
+                     const float *u, double temp, int32_t *out, int32_t *accepted, int32_t *status,
                      void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus

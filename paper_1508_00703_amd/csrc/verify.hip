@@ -680,10 +680,10 @@ extern "C" int pdb_draft_verify_workspace_bytes(int64_t b, int32_t k, int64_t v,
 
 extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *draft, int64_t ldq,
                                 int dtype, int64_t b, int32_t k, int64_t v, const void *tokens,
-                                int index, const float *u, float temp, int32_t *out,
+                                int index, const float *u, double temp, int32_t *out,
                                 int32_t *accepted, int32_t *status, void *ws, size_t ws_bytes,
                                 hipStream_t stream) {
-    if (b < 0 || k < 0 || v <= 0 || !good_temp(temp)) return PDB_ERR_INVALID_ARG;
+    if (b < 0 || k < 0 || v <= 0 || !(temp > 0.0) || !good_temp((float)temp)) return PDB_ERR_INVALID_ARG;
     if (k > PDB_MAX_DRAFT || b > INT32_MAX || b * (k + 1) > INT32_MAX) return PDB_ERR_UNSUPPORTED;
     if (int e = check_matrix(target, dtype, ldt, b * (k + 1), v)) return e;
     if (draft)
@@ -698,9 +698,9 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
     if (b * sp.chunks > INT32_MAX) return PDB_ERR_UNSUPPORTED;
     Verify p = {};
     p.target = target, p.draft = k > 0 ? draft : nullptr, p.tokens = tokens, p.ldt = ldt, p.ldq = ldq;
-    p.v = v, p.b = (int32_t)b, p.k = k, p.index = index, p.u = u, p.inv_t = 1.0 / (double)temp;
+    p.v = v, p.b = (int32_t)b, p.k = k, p.index = index, p.u = u, p.inv_t = 1.0 / temp;
     p.by = p.inv_t * 0x1.71547652b82fep+6;
-    p.c = kLog2e / temp;
+    p.c = (float)(0x1.71547652b82fep+0 / temp);
     p.out = out, p.accepted = accepted, p.status = status, p.chunks = sp.chunks;
     char *at = static_cast<char *>(ws);
     p.part = reinterpret_cast<Sum *>(at);

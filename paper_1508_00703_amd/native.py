@@ -169,8 +169,8 @@ def load() -> ctypes.CDLL:
     lib.pdb_distill.argtypes = [P, i32, i64, i64, i64, P, P, i32, i32, f32, P, P, P, i64, P, P, sz,
                                 P]
     lib.pdb_draft_verify_workspace_bytes.argtypes = [i64, i32, i64, ctypes.POINTER(sz)]
-    lib.pdb_draft_verify.argtypes = [P, i64, P, i64, i32, i64, i32, i64, P, i32, P, f32, P, P, P, P,
-                                     sz, P]
+    lib.pdb_draft_verify.argtypes = [P, i64, P, i64, i32, i64, i32, i64, P, i32, P, ctypes.c_double, P,
+                                     P, P, P, sz, P]
     lib.pdb_gated_scan_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
     lib.pdb_gated_scan.argtypes = [P, i64, P, i64, i32, i64, i64, P, i64, P, P, i64, P, P, P, P, sz, P]
     lib.pdb_gated_scan_grad.argtypes = [P, i64, P, i64, P, i64, i32, i64, i64, P, i64, P, P, P, P,

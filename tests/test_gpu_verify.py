@@ -33,7 +33,7 @@ def same(gpu, t, t64, q, q64, x, u, temp=1.0, index=None):
     tok = torch.from_numpy(x).to(gpu, index or torch.int32) if k else None
     status = torch.zeros(1, dtype=torch.int32, device=gpu)
     r = native.pdb_draft_verify(t, u, tokens=tok, draft=q if k else None, temp=temp, status=status)
-    out, acc = ref.verify(t64, q64 if q is not None else None, x, f64(u), float(np.float32(temp)))
+    out, acc = ref.verify(t64, q64 if q is not None else None, x, f64(u), temp)
     assert np.array_equal(r.tokens.cpu().numpy(), out)
     assert np.array_equal(r.accepted.cpu().numpy(), acc)
     return r, int(status)
@@ -151,21 +151,31 @@ def test_drawn_tokens_follow_the_distribution(gpu):
     assert float((got - torch.softmax(z[0].double(), 0)).abs().max()) < 5 * (0.25 / n) ** 0.5
 
 
-def test_near_borders(gpu):
-    """Random numbers a part in 1e7 to either side of a border of the running sum."""
+@pytest.mark.parametrize("temp", [1.0, 0.7])
+def test_near_borders(gpu, temp):
+    """Random numbers a part in 1e7 to either side of a border of the running sum, and a
+    vocabulary in which many borders lie as near to a number as a temperature of 32 bits
+    would move them."""
     import torch
 
     rng = np.random.default_rng(6)
+    n, v = 4000, 131_072
+    row, row64 = on_gpu(rng.normal(size=(1, v)), "f16", gpu)
+    run = np.cumsum(ref.softmax(row64[0], temp))
+    u = rng.random(n).astype(np.float32)
+    got = native_mod().pdb_draft_verify(row.expand(n, v).contiguous(), torch.from_numpy(u[:, None]).to(gpu), temp=temp)
+    assert np.array_equal(got.tokens[:, 0].cpu().numpy(),
+                          np.searchsorted(run, u.astype(np.float64) * run[-1], side="right"))
     v, n = 4500, 400
     z = np.repeat(rng.normal(size=(1, v)).astype(np.float32), n, 0)
     t, t64 = on_gpu(z, "f32", gpu)
-    run = np.cumsum(ref.softmax(t64[0], 1.0))
+    run = np.cumsum(ref.softmax(t64[0], temp))
     at = np.sort(rng.choice(v, n // 2, replace=False))
     edge = run[at].astype(np.float32)
     u = np.concatenate([np.nextafter(edge, np.float32(0)), np.nextafter(edge, np.float32(1))])
     u = np.minimum(u, np.float32(1 - 2 ** -24))
     same(gpu, t, t64.reshape(n, 1, v), None, None, np.zeros((n, 0), np.int64),
-         torch.from_numpy(u[:, None]).to(gpu))
+         torch.from_numpy(u[:, None]).to(gpu), temp)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
