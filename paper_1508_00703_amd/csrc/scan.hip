@@ -6,22 +6,22 @@
 // hold, and the channels into strips of 128 bytes of a row: a block has a tile of a strip
 // in registers, some rows of a vector of channels to a thread, and reads it once.  The
 // threads' maps are joined through LDS, the tiles' through the workspace while the blocks
-// run: each publishes its map, waits for the state behind the tile kReach before and
-// applies the maps between, in order (so the sums do not depend on who was first), and
+// run: each publishes its map, waits for the state behind the tile REACH before and
+// applies the maps between, in thirds (so the sums do not depend on who was first), and
 // publishes the state behind its own.  Tiles are dealt by a counter, so a block waits
 // only for blocks that have begun.  A row that begins a sequence takes its first state in
 // place of what enters: its map is "cut", a = -0 (gates are never negative, so products
 // and selects keep the mark), and nothing of another sequence passes it, not even a NaN.
 //
-// The bound is the bytes.  131,072 rows of 1,024 channels in 16 bits take 170 us, 4.7 TB/s
-// (two launches that read the rows twice: 504), the gradient's 65,536 158 us, 4.2 TB/s.
+// The bound is the bytes.  131,072 rows of 1,024 channels in 16 bits take 168 us, 4.8 TB/s
+// (two launches that read the rows twice: 504), the gradient's 65,536 156 us, 4.3 TB/s.
 // What stands before the bytes:
-// * waiting: for a tile's loads, its join, and the chain, 0.1 us a tile of one strip alone;
-//   without the chain's waits the same rows took 168 us, but 32,768 of 2,048 channels 95
-//   where they take 105, since a late tile delays those behind it.  Tiles of half the rows
-//   took a third longer, the latencies being a tile's whatever its size.
+// * waiting: for a tile's loads, its join, and the chain.  Without the chain's waits the
+//   same rows took as long, but 32,768 of 2,048 channels 95 us where they take 102, since a
+//   late tile delays those behind it.  Tiles of half the rows took a third longer, the
+//   latencies being a tile's whatever its size.
 // * the vector unit, 12 operations and two transcendental ones an element and pass: gates
-//   that cost nothing would save 10 us of the 105.
+//   that cost nothing would save 10 us of the 102.
 // * registers: two numbers an element (the map behind each row) keep the forward pass of 16
 //   bits at two blocks a unit.  Loading the next tile's rows under the chain, or keeping
 //   x and gate and computing gates twice, for three blocks, gained nothing.
@@ -36,7 +36,7 @@ constexpr int kStripLanes = 8;                   // lanes over 128 bytes of a ro
 constexpr int kRowLanes = kBlock / kStripLanes;  // 32
 
 // Rows of a thread: two numbers an element, in the backward four.  (In the backward, eight
-// rows of 16 bits spill: 237 us where four take 164.)
+// rows of 16 bits spill: 237 us where four take 160.)
 template <int DT, bool BACK>
 struct Shape {
     static constexpr int V = Elem<DT>::kVec;
@@ -407,7 +407,13 @@ __device__ __forceinline__ uint32_t deal(const Scan &p) {
     return w;
 }
 
-constexpr int kReach = 16;  // tiles that a hop of the chain passes
+// Tiles that a hop of the chain passes, each of them a map that the block fetches: of few
+// strips more, where the chain is all that takes time (131,072 rows of 16 bits: of 64
+// channels 40 us with 16, 26 with 49; of 128 43 and 35; of 256 56 and 59; of 1,024 168 and
+// 182.  The gradient of 65,536 rows: of 64 channels 48 and 28, of 256 66 and 59, of 512 92
+// and 103).
+constexpr int kReach = 16, kFarReach = 49;
+constexpr int64_t kFewStrips = 2, kFewStripsBack = 4;
 constexpr int64_t kPatience = 2000000000;  // ticks of the 100 MHz clock: 20 s
 constexpr int64_t kUneasy = 100000;       // 1 ms
 
@@ -457,19 +463,20 @@ struct Link {
     }
 };
 
-// What the waves of a block fetch of the chain: the maps of the kReach - 1 tiles before
-// its own, a third of them to each of three waves.
-template <int V>
+// What the waves of a block fetch of the chain: the maps of the REACH - 1 tiles before
+// its own, a third of them to each of three waves, which makes one map of them.
+template <int V, int REACH>
 struct Fetched {
-    static constexpr int kEach = (kReach - 1) / 3;
-    static_assert(3 * kEach == kReach - 1, "thirds");
-    unsigned long long map[kReach - 1][kStripLanes * V];
+    static constexpr int kEach = (REACH - 1) / 3;
+    static_assert(3 * kEach == REACH - 1, "thirds");
+    Map map[3][kStripLanes * V];  // the nearest third first
     float leave[kStripLanes * V];
     int late, cut;  // a wait given up; a cut among the maps, so that no state is waited for
 };
-template <int V>
-__device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, int third, Fetched<V> &f) {
-    constexpr int kEach = Fetched<V>::kEach;
+template <int V, int REACH>
+__device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, int third,
+                                           Fetched<V, REACH> &f) {
+    constexpr int kEach = Fetched<V, REACH>::kEach;
     if (!p.ticket) return;
     const Link<V> l(p, turn, strip);
     const int64_t t0 = now_ticks();
@@ -478,7 +485,7 @@ __device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, i
         bool missing = false;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            // (maps of no tile are not asked for: they are not applied)
+            // (maps of no tile are neither asked for nor applied)
             const int back = third * kEach + j + 1;
             w[j] = back <= turn ? peek(p.total + (l.at - back * l.slots)) : 0ull;
         }
@@ -491,29 +498,29 @@ __device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, i
         }
         __builtin_amdgcn_s_sleep(1);
     }
-    bool cut = false;
+    Map m = {1.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        f.map[third * kEach + j][slot_of<V>()] = w[j];
-        cut |= third * kEach + j < turn && is_cut(map_of(w[j]).a);
-    }
+    for (int j = kEach - 1; j >= 0; --j)
+        if (third * kEach + j < turn) m = then(m, map_of(w[j]));
+    f.map[third][slot_of<V>()] = m;
     // (a tile with a sequence's beginning has cuts in all its slots)
-    if (__all(cut)) __hip_atomic_store(&f.cut, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    if (__all(is_cut(m.a))) __hip_atomic_store(&f.cut, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
-// The block's own map, and the state behind the tile kReach before.
-template <int V>
-__device__ __forceinline__ void chain_wait(const Scan &p, int turn, int strip, Map m, Fetched<V> &f) {
+// The block's own map, and the state behind the tile REACH before.
+template <int V, int REACH>
+__device__ __forceinline__ void chain_wait(const Scan &p, int turn, int strip, Map m,
+                                           Fetched<V, REACH> &f) {
     if (!p.ticket) return;
     const Link<V> l(p, turn, strip);
     if (turn < p.tiles - 1 && l.mine) post(p.total + l.at, word_of(m));
     const bool cut = __all(is_cut(m.a));  // what leaves the tile does not hang on what enters
-    if (cut && turn + kReach < p.tiles && l.mine) post(p.leave + l.at, word_of(m.c));
+    if (cut && turn + REACH < p.tiles && l.mine) post(p.leave + l.at, word_of(m.c));
     uint32_t h = 0;
-    if (turn >= kReach) {
+    if (turn >= REACH) {
         const int64_t t0 = now_ticks();
         while (true) {
-            h = peek(p.leave + (l.at - kReach * l.slots));
+            h = peek(p.leave + (l.at - REACH * l.slots));
             if (!__any(h == ~0u)) break;
             if (__hip_atomic_load(&f.cut, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)) break;
             if (__any(give_up(p, t0))) {
@@ -527,20 +534,19 @@ __device__ __forceinline__ void chain_wait(const Scan &p, int turn, int strip, M
 }
 // What enters the tile, from both, by every wave; `first`, one of them, publishes the state
 // behind the tile, whose map is m.  A wait that was given up ends with NaN and a status.
-template <int V>
+template <int V, int REACH>
 __device__ __forceinline__ float chain_end(const Scan &p, int turn, int strip, Map m, bool first,
-                                           const Fetched<V> &f) {
+                                           const Fetched<V, REACH> &f) {
     if (!p.ticket) return 0.0f;
     float h = f.leave[slot_of<V>()];
 #pragma unroll
-    for (int j = kReach - 2; j >= 0; --j)
-        if (j < turn) h = apply(map_of(f.map[j][slot_of<V>()]), h);
+    for (int j = 2; j >= 0; --j) h = apply(f.map[j][slot_of<V>()], h);
     if (f.late) {
         h = kNan;  // seen by whoever uses the result
         if (p.status) *p.status = PDB_ERR_DEVICE;
     }
     const Link<V> l(p, turn, strip);
-    if (first && !is_cut(m.a) && turn + kReach < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
+    if (first && !is_cut(m.a) && turn + REACH < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
     return h;
 }
 
@@ -555,14 +561,14 @@ __device__ __forceinline__ void either(bool plain, F f) {
         f(std::false_type());
 }
 
-template <int DT, bool WIDE>
+template <int DT, bool WIDE, int REACH>
 __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
     using S = Shape<DT, false>;
     using At = Place<DT, WIDE, false>;
     constexpr int V = S::V, R = S::kRows;
     __shared__ Joint<V, false> s;
     __shared__ Edges<S::kTileRows> e;
-    __shared__ Fetched<V> fetched;
+    __shared__ Fetched<V, REACH> fetched;
     const int wave = __builtin_amdgcn_readfirstlane(wave_in_block());
     check_starts(p);
     if (wave == 0) {
@@ -628,11 +634,11 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
     __syncthreads();
     const Map m = s.total();
     if (wave == 0)
-        chain_wait<V>(p, at.turn, at.strip, m, fetched);
+        chain_wait<V, REACH>(p, at.turn, at.strip, m, fetched);
     else
-        fetch_maps<V>(p, at.turn, at.strip, wave - 1, fetched);
+        fetch_maps<V, REACH>(p, at.turn, at.strip, wave - 1, fetched);
     __syncthreads();
-    s.spread(wave, chain_end<V>(p, at.turn, at.strip, m, wave == 0, fetched));
+    s.spread(wave, chain_end<V, REACH>(p, at.turn, at.strip, m, wave == 0, fetched));
     float h[V];
     s.get(at.rl, at.cl, h);
     if (!at.act) return;
@@ -664,15 +670,15 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
 // ask of the state before them) as e -> f (dy + e); a row that ends a sequence takes
 // d_state in place of e.  The states come from the mark that the tile begins with, so
 // that only e passes along the chain.
-template <int DT, bool WIDE>
-__global__ __launch_bounds__(kBlock, 3) void k_scan_grad(Scan p) {
+template <int DT, bool WIDE, int REACH>
+__global__ __launch_bounds__(kBlock, REACH == kReach ? 3 : 2) void k_scan_grad(Scan p) {
     using S = Shape<DT, true>;
     using At = Place<DT, WIDE, true>;
     constexpr int V = S::V, R = S::kRows;
     __shared__ Joint<V, false> forth;
     __shared__ Joint<V, true> back;
     __shared__ Edges<S::kTileRows> e;
-    __shared__ Fetched<V> fetched;
+    __shared__ Fetched<V, REACH> fetched;
     const int wave = __builtin_amdgcn_readfirstlane(wave_in_block());
     check_starts(p);
     if (wave == 0) {
@@ -759,14 +765,14 @@ __global__ __launch_bounds__(kBlock, 3) void k_scan_grad(Scan p) {
     __syncthreads();
     const Map m = back.total();
     if (wave == 0)
-        chain_wait<V>(p, at.turn, at.strip, m, fetched);
+        chain_wait<V, REACH>(p, at.turn, at.strip, m, fetched);
     else
-        fetch_maps<V>(p, at.turn, at.strip, wave - 1, fetched);
+        fetch_maps<V, REACH>(p, at.turn, at.strip, wave - 1, fetched);
     float h[V], g[V];
     forth.spread(wave, mark);
     forth.get(at.rl, at.cl, h);
     __syncthreads();
-    back.spread(wave, chain_end<V>(p, at.turn, at.strip, m, wave == 0, fetched));
+    back.spread(wave, chain_end<V, REACH>(p, at.turn, at.strip, m, wave == 0, fetched));
     back.get(at.rl, at.cl, g);
     if (!at.act) return;
     either(plain, [&](auto is_plain) {
@@ -907,10 +913,18 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
                 k_scan_clear<<<grid_for(std::max(words / 4, cut.tiles * kWave), kBlock, 2048), kBlock, 0,
                                stream>>>(p, words, Shape<DT, GRAD>::kTileRows);
             }
-            if constexpr (GRAD)
-                k_scan_grad<DT, W><<<grid, kBlock, 0, stream>>>(p);
-            else
-                k_scan<DT, W><<<grid, kBlock, 0, stream>>>(p);
+            const bool few = cut.tiles > kReach && cut.strips <= (GRAD ? kFewStripsBack : kFewStrips);
+            if constexpr (GRAD) {
+                if (few)
+                    k_scan_grad<DT, W, kFarReach><<<grid, kBlock, 0, stream>>>(p);
+                else
+                    k_scan_grad<DT, W, kReach><<<grid, kBlock, 0, stream>>>(p);
+            } else {
+                if (few)
+                    k_scan<DT, W, kFarReach><<<grid, kBlock, 0, stream>>>(p);
+                else
+                    k_scan<DT, W, kReach><<<grid, kBlock, 0, stream>>>(p);
+            }
             PDB_LAUNCHED();
             return PDB_OK;
         };
