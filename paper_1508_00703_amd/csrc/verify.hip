@@ -509,19 +509,35 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
     __shared__ Powers e;
     __shared__ int todo, list[kBlock];
     const int64_t i = blockIdx.x;
-    const Choice c = p.choice[i];
     Chunk *chunk = p.chunk + i * p.chunks;
     const int t = threadIdx.x;
-    const int64_t each = (p.chunks + kBlock - 1) / kBlock, k0 = min(t * each, p.chunks),
+    // Up to 64 chunks are a wave's, each wave going over all of them, which spares the
+    // block's waits; else a stretch of them is a thread's.  Where that is one, it stays in
+    // registers.
+    const bool narrow = p.chunks <= kWave;
+    const int id = narrow ? lane_id() : t, ids = narrow ? kWave : kBlock;
+    const int64_t each = (p.chunks + ids - 1) / ids, k0 = min(id * each, p.chunks),
                   k1 = min(k0 + each, p.chunks);
-    e.fill();
-    __syncthreads();
-    // (of up to kBlock chunks each thread keeps its own)
+    // all that is known from the start is asked for first
     __shared__ double redone[kBlock];
     const bool single = each == 1;
     Chunk own = {};
     if (single && k0 < k1) own = chunk[k0];
+    const double number = (double)p.u[i * (p.k + 1) + p.k];
+    const Choice c = p.k == 0 ? Choice{0.0, 0.0, 0.0, 0, -1} : p.choice[i];
+    int32_t token = -1;
+    if (t < p.k) token = read_token(p.tokens, p.index, i * p.k + t, p.v, nullptr);
+    const int have = drafted(p, i);
+    e.fill();
+    __syncthreads();
     auto at = [&](int64_t k) { return single ? own : chunk[k]; };
+    auto sum_of = [&](double v) { return narrow ? wave_sum_f64(v) : block_sum_f64(v); };
+    auto before_of = [&](double v, double *all) {
+        if (!narrow) return block_before_f64(v, all);
+        const double b = wave_before_f64(v);
+        *all = __shfl(b + v, kWave - 1);
+        return b;
+    };
     // the row's maximum, where chunks have their own
     double m = c.mp;
     if (p.k == 0) {
@@ -530,20 +546,22 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
         for (int64_t k = k0; k < k1; ++k) m = fmax(m, at(k).m);
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o));
-        if (lane_id() == 0) tops[wave_in_block()] = m;
-        __syncthreads();
-        m = fmax(fmax(tops[0], tops[1]), fmax(tops[2], tops[3]));
+        if (!narrow) {
+            if (lane_id() == 0) tops[wave_in_block()] = m;
+            __syncthreads();
+            m = fmax(fmax(tops[0], tops[1]), fmax(tops[2], tops[3]));
+        }
     }
     auto mass_p = [&](const Chunk &h) { return p.k == 0 ? h.sp * e.exp(h.m, m, p.by) : h.sp; };
     double sum = 0.0, sq = 0.0, all = 0.0;
     for (int64_t k = k0; k < k1; ++k) sum += mass_p(at(k)), sq += at(k).sq;
-    const double before_p = block_before_f64(sum, &all);
+    const double before_p = before_of(sum, &all);
     bool residual = c.x >= 0;
     double r = 0.0, before = before_p;
     const double all_p = all;
     if (residual) {
         if (p.draft) {
-            sq = block_sum_f64(sq);
+            sq = sum_of(sq);
             r = sq == 0.0 ? 0.0 : all_p / sq;
             if (!(sq >= 0.0)) residual = false;  // the draft's row has no distribution
         }
@@ -557,7 +575,7 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
         for (int64_t a = 0; a < each; ++a) {
             if (t == 0) todo = 0;
             __syncthreads();
-            if (k0 + a < k1 && again(k0 + a)) list[atomicAdd(&todo, 1)] = t;
+            if (t < ids && k0 + a < k1 && again(k0 + a)) list[atomicAdd(&todo, 1)] = t;
             __syncthreads();
             for (int n = 0; n < todo; ++n) {
                 const int64_t k = list[n] * each + a;
@@ -587,14 +605,14 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
     if (residual) {
         double s = 0.0;
         for (int64_t k = k0; k < k1; ++k) s += mass(k);
-        before = block_before_f64(s, &all);
+        before = before_of(s, &all);
         if (!(all > 0.0)) {
             residual = false;
             before = before_p;
             all = all_p;
         }
     }
-    const double bar = (double)p.u[i * (p.k + 1) + p.k] * all;
+    const double bar = number * all;
     constexpr int64_t kNone = INT64_MAX;
     int64_t found = kNone, last = -1;
     double run = before, base = before;
@@ -605,10 +623,18 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
         if (w > 0.0) last = k;
     }
     int64_t chunk_found = found, chunk_last = last;
-    block_ends_i64(chunk_found, chunk_last);
-    __shared__ double s_base;
-    if (found == chunk_found && found != kNone) s_base = base;
-    __syncthreads();
+    if (narrow) {
+        const unsigned long long f = __ballot(found != kNone), l = __ballot(last >= 0);
+        chunk_found = f ? __ffsll(f) - 1 : kNone;
+        chunk_last = l ? 63 - __clzll(l) : -1;
+        base = __shfl(base, f ? (int)chunk_found : 0);
+    } else {
+        __shared__ double s_base;
+        block_ends_i64(chunk_found, chunk_last);
+        if (found == chunk_found && found != kNone) s_base = base;
+        __syncthreads();
+        base = s_base;
+    }
     int64_t next = -1;
     if (chunk_last >= 0 && all_p >= 0.0) {  // (not of a row with a NaN)
         // a sum that none exceeds: the last weight above 0
@@ -619,7 +645,7 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
         weights<DT, E>(p, c, i, e0, m, r, residual, e, w);
 #pragma unroll
         for (int q = 0; q < E; ++q) s += w[q];
-        double sofar = (chunk_found != kNone ? s_base : 0.0) + block_before_f64(s, &total);
+        double sofar = (chunk_found != kNone ? base : 0.0) + block_before_f64(s, &total);
         int64_t hit = kNone, end = -1;
 #pragma unroll
         for (int q = 0; q < E; ++q) {
@@ -633,13 +659,8 @@ __global__ __launch_bounds__(kBlock) void k_verify_pick(Verify p) {
         // the chunk's sum and its entries' may differ in their last bits
         next = hit != kNone ? hit : end;
     }
-    for (int j = t; j <= p.k; j += kBlock) {
-        int32_t o = -1;
-        if (j < c.at) o = read_token(p.tokens, p.index, i * p.k + j, p.v, nullptr);
-        if (j == c.at) o = (int32_t)next;
-        p.out[i * (p.k + 1) + j] = o;
-    }
-    const int have = drafted(p, i);
+    if (t <= p.k) p.out[i * (p.k + 1) + t] = t < c.at ? token : t == c.at ? (int32_t)next : -1;
+    static_assert(PDB_MAX_DRAFT < kBlock, "a place to a thread");
     if (t == 0 && have < p.k) read_token(p.tokens, p.index, i * p.k + have, p.v, p.status);
     if (t == 0) p.accepted[i] = c.at;
 }
