@@ -463,6 +463,11 @@ struct Link {
     }
 };
 
+// Whether what leaves a tile does not hang on what enters it, in any slot of the strip: the
+// state behind it is published with its map then.  (Not slot by slot: a gate that is no
+// number hides a cut, and each slot is published once, here or in chain_end.)
+__device__ __forceinline__ bool all_cut(Map m) { return __all(is_cut(m.a)); }
+
 // What the waves of a block fetch of the chain: the maps of the REACH - 1 tiles before
 // its own, a third of them to each of three waves, which makes one map of them.
 template <int V, int REACH>
@@ -504,7 +509,7 @@ __device__ __forceinline__ void fetch_maps(const Scan &p, int turn, int strip, i
         if (third * kEach + j < turn) m = then(m, map_of(w[j]));
     f.map[third][slot_of<V>()] = m;
     // (a tile with a sequence's beginning has cuts in all its slots)
-    if (__all(is_cut(m.a))) __hip_atomic_store(&f.cut, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    if (all_cut(m)) __hip_atomic_store(&f.cut, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
 // The block's own map, and the state behind the tile REACH before.
@@ -514,8 +519,7 @@ __device__ __forceinline__ void chain_wait(const Scan &p, int turn, int strip, M
     if (!p.ticket) return;
     const Link<V> l(p, turn, strip);
     if (turn < p.tiles - 1 && l.mine) post(p.total + l.at, word_of(m));
-    const bool cut = __all(is_cut(m.a));  // what leaves the tile does not hang on what enters
-    if (cut && turn + REACH < p.tiles && l.mine) post(p.leave + l.at, word_of(m.c));
+    if (all_cut(m) && turn + REACH < p.tiles && l.mine) post(p.leave + l.at, word_of(m.c));
     uint32_t h = 0;
     if (turn >= REACH) {
         const int64_t t0 = now_ticks();
@@ -546,7 +550,7 @@ __device__ __forceinline__ float chain_end(const Scan &p, int turn, int strip, M
         if (p.status) *p.status = PDB_ERR_DEVICE;
     }
     const Link<V> l(p, turn, strip);
-    if (first && !is_cut(m.a) && turn + REACH < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
+    if (first && !all_cut(m) && turn + REACH < p.tiles && l.mine) post(p.leave + l.at, word_of(apply(m, h)));
     return h;
 }
 

@@ -1113,9 +1113,11 @@ def pdb_grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, step: fl
     if out is not grads and list(map(_SHAPE_OF, out)) != list(map(_SHAPE_OF, grads)):
         raise ValueError("out must hold a tensor of the same shape for every gradient")
     g = o = _tensors(grads, "grads", dev)[0]
-    some = [p for p in map(torch.Tensor.data_ptr, out) if p]
-    if len(set(some)) != len(some):
-        raise ValueError("a tensor is written twice")
+    at = list(map(torch.Tensor.data_ptr, out))
+    if len(set(at)) != len(at):
+        at = [t.data_ptr() for t in out if t.numel()]
+        if len(set(at)) != len(at):
+            raise ValueError("a tensor is written twice")
     if out is not grads:
         o, apart = _tensors(out, "out", dev, g)
         if apart:  # rows further apart than their columns: the gradients by rows, too

@@ -199,6 +199,34 @@ def test_values_that_are_not_finite_stay_in_their_sequence(gpu, bad):
     assert ok.all() and np.isfinite(f64(r.dx)).all()
 
 
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("d", [24, 600])
+def test_gates_that_are_not_finite(gpu, bad, d):
+    """A gate that is no number behind a sequence's first row, many tiles before the end:
+    its channel only, to the end of its sequence, forth and back."""
+    import torch
+
+    native = native_mod()
+    n = 12_000
+    starts = torch.tensor([0, 900, 1000, 5000, 5001, n], dtype=torch.int32, device=gpu)
+    x, g, dy = torch.randn(3, n, d, device=gpu)
+    want = native.pdb_gated_scan(x, g, starts=starts, marks=True)
+    back = native.pdb_gated_scan_grad(dy, x, g, want.marks, starts=starts)
+    g[1010, 3] = g[5003, 7] = bad
+    status = torch.zeros(1, dtype=torch.int32, device=gpu)
+    f = native.pdb_gated_scan(x, g, starts=starts, marks=True, status=status)
+    r = native.pdb_gated_scan_grad(dy, x, g, f.marks, starts=starts, status=status)
+    assert int(status) == 0
+    for got, ref_, name in ((f.y, want.y, "y"), (r.dx, back.dx, "dx"), (r.dgate, back.dgate, "dgate")):
+        same = got == ref_
+        for c, a, b in ((3, 1010, 5000), (7, 5003, n)):
+            lo, hi = (a, b) if name == "y" else (1000 if c == 3 else 5001, b)
+            if np.isnan(bad) and name == "y":
+                assert not torch.isfinite(got[lo:hi, c]).any()
+            same[lo:hi, c] = True
+        assert bool(same.all()), name
+
+
 def test_gates_at_their_ends(gpu):
     """Gates of +-inf and far out: the state is kept, or taken from the input, exactly."""
     import torch
@@ -409,6 +437,8 @@ def test_layouts_that_differ(gpu):
     with pytest.raises(ValueError, match="twice"):
         native.pdb_grad_clip([w, w], 1.0)
     assert abs(float(native.pdb_grad_norm([w, w])) / 48 ** 0.5 - 1) < 1e-6   # to read twice is no harm
+    native.pdb_grad_clip([w, w[:0], w[:0]], 1.0)   # nothing is written at the same address
+    assert abs(float(native.pdb_grad_norm([w])) - 1) < 1e-6
 
 
 def test_captured_layers(gpu):
