@@ -43,12 +43,14 @@ int pdb_gated_scan_workspace_bytes(int64_t n, int64_t d, size_t *bytes);
  * ceil(n / PDB_SCAN_MARK) x d float without gaps, or NULL: row i is the h that
  * enters row i * PDB_SCAN_MARK, for pdb_gated_scan_grad (unspecified where that
  * row is of no sequence).
- * A value that is not finite makes its channel not finite from its row to its
- * sequence's end, and reaches no other sequence.
- * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8
- * (NULL in the decoding step: n = b, no starts), for this call alone until it has run (tiles of rows pass their states through it; a
- * wait of 20 s there, which only a workspace that something else writes brings about,
- * ends with NaN and *status = PDB_ERR_DEVICE). */
+ * A NaN, or an infinite x or h0, makes its channel not finite from its row to its
+ * sequence's end, and reaches no other sequence.  Infinite gates keep the state, or
+ * take the input.
+ * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8,
+ * for this call alone until it has run; NULL in the decoding step (n = b, no starts).
+ * Tiles of rows pass their states through it: a wait of 20 s there, which only a
+ * workspace that something else writes brings about, ends with NaN and *status =
+ * PDB_ERR_DEVICE. */
 int pdb_gated_scan(const void *x, int64_t ldx, const void *gate, int64_t ldg, int dtype, int64_t n,
                    int64_t d, const int32_t *starts, int64_t b, const float *h0, void *y,
                    int64_t ldy, float *state, float *marks, int32_t *status, void *ws,

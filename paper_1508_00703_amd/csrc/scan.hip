@@ -14,7 +14,7 @@
 // and selects keep the mark), and nothing of another sequence passes it, not even a NaN.
 //
 // The bound is the bytes.  131,072 rows of 1,024 channels in 16 bits take 168 us, 4.8 TB/s
-// (two launches that read the rows twice: 504), the gradient's 65,536 156 us, 4.3 TB/s.
+// (in launches that read the rows twice: 504), the gradient's 65,536 156 us, 4.3 TB/s.
 // What stands before the bytes:
 // * waiting: for a tile's loads, its join, and the chain.  Without the chain's waits the
 //   same rows took as long, but 32,768 of 2,048 channels 95 us where they take 102, since a

@@ -731,7 +731,8 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
         constexpr int DT = decltype(dt)::value;
         if (k > 0) {
             const int64_t rows = b * (k + 1) + (p.draft ? b * k : 0);
-            const int64_t tile = kTileVecs * kBlock, tiles = std::max<int64_t>(cdiv(v / Elem<DT>::kVec, tile), 1);
+            const int64_t tile = kTileVecs * kBlock;
+            const int64_t tiles = std::max<int64_t>(cdiv(v / Elem<DT>::kVec, tile), 1);
             const int64_t parts = std::min(std::min(kWantParts / rows, tiles), kMostParts);
             const int64_t of_part = cdiv(tiles, std::max<int64_t>(parts, 1));
             p.parts = (int32_t)cdiv(tiles, of_part);
