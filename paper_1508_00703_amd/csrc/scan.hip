@@ -60,15 +60,18 @@ __device__ __forceinline__ Map then(Map first, Map second) {
 }
 
 // f = 1 / (1 + e^-g) and k = 1 - f, each with its own relative accuracy at either end.
+// From t = 2^126 on (g below -87.3) 1 / (1 + t) is no normal number and the reciprocal
+// gives 0: f is 0 there, to within 2^-126, but k is 1.  So k = t f is taken with an f of at
+// least 2^-126, which leaves it within its rounding below t = 2^102 and makes it 1 or more,
+// up to infinity, where f was 0; in between the product is 1 but for rounding.
 struct Gate {
     float f, k;
 };
 __device__ __forceinline__ Gate gate_of(float g) {
     const float t = exp2_raw(g * -kLog2e);
     const float f = __builtin_amdgcn_rcpf(1.0f + t);
-    // (an infinite t: f = 0 and t f no number, of which fmin takes the 1; a gate that is no
-    // number stays one in f)
-    return {f, fminf(t * f, 1.0f)};
+    // (a gate that is no number stays one in f)
+    return {f, fminf(t * fmaxf(f, 0x1p-126f), 1.0f)};
 }
 
 struct Scan {
