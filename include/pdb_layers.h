@@ -65,7 +65,8 @@ int pdb_gated_scan(const void *x, int64_t ldx, const void *gate, int64_t ldg, in
  * (d_state for an empty sequence).  The h are computed again, in binary32, from x,
  * gate, h0 and the marks that pdb_gated_scan gave for the same x, gate, starts and
  * h0.  All matrices are of `dtype`.  Rows of no sequence are left as they were in
- * dx and dgate; status and ws as there. */
+ * dx and dgate.  A NaN among the gates or dy makes dx, dgate and dh0 of its channel NaN
+ * from its row to its sequence's beginning; status and ws as there. */
 int pdb_gated_scan_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *gate,
                         int64_t ldg, int dtype, int64_t n, int64_t d, const int32_t *starts,
                         int64_t b, const float *h0, const float *marks, const float *d_state,

@@ -70,8 +70,8 @@ struct Gate {
 __device__ __forceinline__ Gate gate_of(float g) {
     const float t = exp2_raw(g * -kLog2e);
     const float f = __builtin_amdgcn_rcpf(1.0f + t);
-    // (a gate that is no number stays one in f)
-    return {f, fminf(t * fmaxf(f, 0x1p-126f), 1.0f)};
+    // (the minimum that keeps what is no number: neither is k then)
+    return {f, __builtin_elementwise_minimum(t * fmaxf(f, 0x1p-126f), 1.0f)};
 }
 
 struct Scan {

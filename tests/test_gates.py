@@ -157,3 +157,36 @@ def test_sequences(gpu, dtype):
     for name in ("dx", "dgate"):
         check(f64(getattr(r, name)).reshape(shape), want[name], store(dtype, want[name], want["b" + name]), name)
     check(f64(r.dh0), want["dh0"], want["bdh0"], "dh0")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [5, 24, 600])
+def test_a_gate_that_is_no_number(gpu, dtype, d):
+    """What hangs on it is no number either, the gradient by its own row's input among it;
+    the rest keeps its bits."""
+    import torch
+
+    native = native_mod()
+    n, at, col = 3000, 1010, 3
+    starts = torch.tensor([0, 900, 1000, 2500, n], dtype=torch.int32, device=gpu)
+    x, g, dy = (t.to(torch_type(dtype)) for t in torch.randn(3, n, d, device=gpu))
+    h0 = torch.randn(4, d, device=gpu)
+
+    def calls():
+        f = native.pdb_gated_scan(x, g, starts=starts, h0=h0, marks=True)
+        r = native.pdb_gated_scan_grad(dy, x, g, f.marks, starts=starts, h0=h0)
+        step = native.pdb_gated_scan(x, g, batch=n)
+        return dict(y=f.y, state=f.state, dx=r.dx, dgate=r.dgate, dh0=r.dh0, step=step.y)
+
+    want = calls()
+    g[at, col] = np.nan
+    got = calls()
+    lost = {name: torch.zeros_like(t, dtype=torch.bool) for name, t in want.items()}
+    lost["y"][at:2500, col] = lost["state"][2, col] = True     # from its row to the sequence's end
+    lost["dx"][1000:at + 1, col] = lost["dh0"][2, col] = True  # from its row to the beginning
+    lost["dgate"][1000:2500, col] = True                       # before it by e, behind it by h
+    lost["step"][at, col] = True
+    for name, t in got.items():
+        assert torch.equal(t.isnan(), lost[name]), name
+        assert torch.equal(t[~lost[name]], want[name][~lost[name]]), name
