@@ -15,6 +15,9 @@ constexpr int kBlock = 256;              // threads per block for streaming kern
 constexpr int kItems = 16;               // items per thread in tiled kernels
 constexpr int kTile = kBlock * kItems;   // 4096 elements per tile
 constexpr int64_t kAlign = 256;
+// Blocks of kBlock threads that a launch may have: it takes fewer than 2^32 threads, and
+// the runtime does not refuse more of them but drops what does not fit 32 bits.
+constexpr int64_t kMostBlocks = ((int64_t)1 << 32) / kBlock - 1;
 
 // ----------------------------------------------------------------------------
 // host-side error plumbing

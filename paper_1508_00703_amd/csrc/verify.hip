@@ -686,6 +686,56 @@ Space space_of(int64_t b, int32_t k, int64_t v) {
     return s;
 }
 
+// The call for `count` of its sequences, from i on.
+Verify from_sequence(Verify p, int dtype, int64_t i, int64_t count) {
+    p.b = (int32_t)count;
+    p.target = static_cast<const char *>(p.target) + i * (p.k + 1) * p.ldt * dtype_size(dtype);
+    if (p.draft) p.draft = static_cast<const char *>(p.draft) + i * p.k * p.ldq * dtype_size(dtype);
+    if (p.k > 0) p.tokens = static_cast<const char *>(p.tokens) + i * p.k * (p.index == PDB_I64 ? 8 : 4);
+    p.u += i * (p.k + 1);
+    p.out += i * (p.k + 1);
+    p.accepted += i;
+    return p;
+}
+
+template <int DT>
+int run_verify(Verify p, hipStream_t stream) {
+    if (p.k > 0) {
+        const int64_t rows = (int64_t)p.b * (p.k + 1 + (p.draft ? p.k : 0));
+        const int64_t tile = kTileVecs * kBlock;
+        const int64_t tiles = std::max<int64_t>(cdiv(p.v / Elem<DT>::kVec, tile), 1);
+        const int64_t parts = std::min(std::min(kWantParts / rows, tiles), kMostParts);
+        const int64_t of_part = cdiv(tiles, std::max<int64_t>(parts, 1));
+        p.parts = (int32_t)cdiv(tiles, of_part);
+        p.vecs = (int32_t)std::min<int64_t>(of_part * tile, INT32_MAX / 2);
+        k_verify_sums<DT><<<(unsigned)(rows * p.parts), kBlock, 0, stream>>>(p);
+        PDB_LAUNCHED();
+    }
+    // Where a sequence stops is found by each block of its chunks while they are few,
+    // which saves a launch (64 of them: 20 us against 22, 575: 28 against 30), else once
+    // (2,048: 59 against 62; 4,096: 70 against 73).
+    const unsigned blocks = (unsigned)(p.b * p.chunks), rows = (unsigned)p.b;
+    if (p.k == 0) {
+        constexpr int E = each_of(0);
+        k_verify_chunks<DT, E, true><<<blocks, kBlock, 0, stream>>>(p);
+        PDB_LAUNCHED();
+        k_verify_pick<DT, E><<<rows, kBlock, 0, stream>>>(p);
+    } else {
+        constexpr int E = each_of(1);
+        if (blocks <= 1024) {
+            k_verify_chunks<DT, E, true><<<blocks, kBlock, 0, stream>>>(p);
+        } else {
+            k_verify_choose<DT><<<rows, kBlock, 0, stream>>>(p);
+            PDB_LAUNCHED();
+            k_verify_chunks<DT, E, false><<<blocks, kBlock, 0, stream>>>(p);
+        }
+        PDB_LAUNCHED();
+        k_verify_pick<DT, E><<<rows, kBlock, 0, stream>>>(p);
+    }
+    PDB_LAUNCHED();
+    return PDB_OK;
+}
+
 }  // namespace
 }  // namespace pdbk
 
@@ -717,48 +767,24 @@ extern "C" int pdb_draft_verify(const void *target, int64_t ldt, const void *dra
     const Space sp = space_of(b, k, v);
     if (!ws || !aligned_to(ws, 8) || ws_bytes < sp.total) return PDB_ERR_WORKSPACE;
     if (b * sp.chunks > INT32_MAX) return PDB_ERR_UNSUPPORTED;
-    Verify p = {};
-    p.target = target, p.draft = k > 0 ? draft : nullptr, p.tokens = tokens, p.ldt = ldt, p.ldq = ldq;
-    p.v = v, p.b = (int32_t)b, p.k = k, p.index = index, p.u = u, p.inv_t = 1.0 / temp;
-    p.by = p.inv_t * 0x1.71547652b82fep+6;
-    p.c = (float)(0x1.71547652b82fep+0 / temp);
-    p.out = out, p.accepted = accepted, p.status = status, p.chunks = sp.chunks;
+    Verify all = {};
+    all.target = target, all.draft = k > 0 ? draft : nullptr, all.tokens = tokens, all.ldt = ldt, all.ldq = ldq;
+    all.v = v, all.k = k, all.index = index, all.u = u, all.inv_t = 1.0 / temp;
+    all.by = all.inv_t * 0x1.71547652b82fep+6;
+    all.c = (float)(0x1.71547652b82fep+0 / temp);
+    all.out = out, all.accepted = accepted, all.status = status, all.chunks = sp.chunks;
     char *at = static_cast<char *>(ws);
-    p.part = reinterpret_cast<Sum *>(at);
-    p.choice = reinterpret_cast<Choice *>(at + sp.choice);
-    p.chunk = reinterpret_cast<Chunk *>(at + sp.chunk);
+    all.part = reinterpret_cast<Sum *>(at);
+    all.choice = reinterpret_cast<Choice *>(at + sp.choice);
+    all.chunk = reinterpret_cast<Chunk *>(at + sp.chunk);
+    // As many sequences at once as a launch has blocks for, one behind another in the same
+    // workspace (their parts in step 1: kWantParts at most, or one a row).
+    const int64_t at_once = (kMostBlocks - kWantParts) / std::max<int64_t>(sp.chunks, 2 * k + 1);
     return with_dtype(dtype, [&](auto dt) -> int {
-        constexpr int DT = decltype(dt)::value;
-        if (k > 0) {
-            const int64_t rows = b * (k + 1) + (p.draft ? b * k : 0);
-            const int64_t tile = kTileVecs * kBlock;
-            const int64_t tiles = std::max<int64_t>(cdiv(v / Elem<DT>::kVec, tile), 1);
-            const int64_t parts = std::min(std::min(kWantParts / rows, tiles), kMostParts);
-            const int64_t of_part = cdiv(tiles, std::max<int64_t>(parts, 1));
-            p.parts = (int32_t)cdiv(tiles, of_part);
-            p.vecs = (int32_t)std::min<int64_t>(of_part * tile, INT32_MAX / 2);
-            if (rows * p.parts > INT32_MAX) return PDB_ERR_UNSUPPORTED;
-            k_verify_sums<DT><<<(unsigned)(rows * p.parts), kBlock, 0, stream>>>(p);
+        for (int64_t i = 0; i < b; i += at_once) {
+            const Verify p = from_sequence(all, dtype, i, std::min(at_once, b - i));
+            if (int e = run_verify<decltype(dt)::value>(p, stream)) return e;
         }
-        // Where a sequence stops is found by each block of its chunks while they are few,
-        // which saves a launch (64 of them: 20 us against 22, 575: 28 against 30), else once
-        // (2,048: 59 against 62; 4,096: 70 against 73).
-        const unsigned blocks = (unsigned)(b * p.chunks), rows = (unsigned)b;
-        if (k == 0) {
-            constexpr int E = each_of(0);
-            k_verify_chunks<DT, E, true><<<blocks, kBlock, 0, stream>>>(p);
-            k_verify_pick<DT, E><<<rows, kBlock, 0, stream>>>(p);
-        } else {
-            constexpr int E = each_of(1);
-            if (blocks <= 1024) {
-                k_verify_chunks<DT, E, true><<<blocks, kBlock, 0, stream>>>(p);
-            } else {
-                k_verify_choose<DT><<<rows, kBlock, 0, stream>>>(p);
-                k_verify_chunks<DT, E, false><<<blocks, kBlock, 0, stream>>>(p);
-            }
-            k_verify_pick<DT, E><<<rows, kBlock, 0, stream>>>(p);
-        }
-        PDB_LAUNCHED();
         return PDB_OK;
     });
 }
