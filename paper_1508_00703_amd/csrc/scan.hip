@@ -89,7 +89,8 @@ struct Scan {
     const float *marks_in;
     int32_t *status;
     int32_t tiles, strips;
-    // in the order of the chain (the backward's from the last tile on); NULL of one tile
+    // in the order of the chain (the backward's from the last tile on); NULL of one
+    // tile and one launch
     unsigned long long *total;  // [tiles][strips][slots]: the tiles' maps
     uint32_t *leave;            // the same: the states behind them
     uint32_t *ticket;           // [0]: tiles dealt; [1]: 0 once a wait has lasted too long
@@ -837,24 +838,25 @@ __global__ __launch_bounds__(kBlock) void k_scan_clear(Scan p, int64_t words, in
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(kBlock) void k_scan_step(Scan p, int64_t vecs) {
     constexpr int V = Elem<DT>::kVec;
-    const int64_t w = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (w >= p.n * vecs) return;
-    const int64_t i = w / vecs, c = (w - i * vecs) * V;
-    const int64_t c0 = WIDE ? min(c, p.d - V) : c;
-    float x[V], g[V], h[V];
-    unpack<DT>(load_vec<DT, WIDE>(p.x, p.ldx, i, c0, p.d), x);
-    unpack<DT>(load_vec<DT, WIDE>(p.gate, p.ldg, i, c0, p.d), g);
-    load_row<V, WIDE>(p.h0, i, c0, p.d, h);
-    const int own = (int)(c - c0);
-    if (p.marks && i % PDB_SCAN_MARK == 0)
-        store_row<V, WIDE>(p.marks, i / PDB_SCAN_MARK, c0, p.d, own, h);
+    for (int64_t w = (int64_t)blockIdx.x * kBlock + threadIdx.x; w < p.n * vecs;
+         w += (int64_t)gridDim.x * kBlock) {
+        const int64_t i = w / vecs, c = (w - i * vecs) * V;
+        const int64_t c0 = WIDE ? min(c, p.d - V) : c;
+        float x[V], g[V], h[V];
+        unpack<DT>(load_vec<DT, WIDE>(p.x, p.ldx, i, c0, p.d), x);
+        unpack<DT>(load_vec<DT, WIDE>(p.gate, p.ldg, i, c0, p.d), g);
+        load_row<V, WIDE>(p.h0, i, c0, p.d, h);
+        const int own = (int)(c - c0);
+        if (p.marks && i % PDB_SCAN_MARK == 0)
+            store_row<V, WIDE>(p.marks, i / PDB_SCAN_MARK, c0, p.d, own, h);
 #pragma unroll
-    for (int q = 0; q < V; ++q) {
-        const Gate k = gate_of(g[q]);
-        h[q] = __builtin_fmaf(k.f, h[q], k.k * x[q]);
+        for (int q = 0; q < V; ++q) {
+            const Gate k = gate_of(g[q]);
+            h[q] = __builtin_fmaf(k.f, h[q], k.k * x[q]);
+        }
+        store_vec<DT, WIDE>(p.y, p.ldy, i, c0, p.d, own, h);
+        if (p.state) store_row<V, WIDE>(p.state, i, c0, p.d, own, h);
     }
-    store_vec<DT, WIDE>(p.y, p.ldy, i, c0, p.d, own, h);
-    if (p.state) store_row<V, WIDE>(p.state, i, c0, p.d, own, h);
 }
 
 // No rows at all: the states are the first ones, or zeros.
@@ -881,6 +883,10 @@ size_t scan_ws_bytes(int64_t n, int64_t d) {
     return (size_t)scan_bytes(cut_of(n, d, PDB_BF16, true));
 }
 
+// Blocks of a launch; more are dealt to the next one.
+constexpr int64_t kAtOnce = 1 << 20;
+static_assert(kAtOnce <= kMostBlocks, "a launch takes them");
+
 template <bool GRAD>
 int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
     const Cut cut = cut_of(p.n, p.d, dtype, GRAD);
@@ -897,7 +903,7 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
     if (cut.tiles * cut.strips > INT32_MAX) return PDB_ERR_UNSUPPORTED;
     p.tiles = (int32_t)cut.tiles;
     p.strips = (int32_t)cut.strips;
-    if (cut.tiles > 1 && !step) {
+    if ((cut.tiles > 1 || cut.strips > kAtOnce) && !step) {
         p.ticket = static_cast<uint32_t *>(ws);
         p.total = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + kAlign);
         p.leave = reinterpret_cast<uint32_t *>(p.total + cut.tiles * cut.slots);
@@ -907,11 +913,9 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
         constexpr int DT = decltype(dt)::value;
         auto go = [&](auto wide) -> int {
             constexpr bool W = decltype(wide)::value;
-            const unsigned grid = (unsigned)(cut.tiles * cut.strips);
             if (step) {
                 const int64_t vecs = cdiv(p.d, Elem<DT>::kVec);
-                if (cdiv(p.n * vecs, kBlock) > INT32_MAX) return PDB_ERR_UNSUPPORTED;
-                k_scan_step<DT, W><<<(unsigned)cdiv(p.n * vecs, kBlock), kBlock, 0, stream>>>(p, vecs);
+                k_scan_step<DT, W><<<grid_for(p.n * vecs, kBlock), kBlock, 0, stream>>>(p, vecs);
                 PDB_LAUNCHED();
                 return PDB_OK;
             }
@@ -919,20 +923,25 @@ int run_scan(Scan p, int dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
                 const int64_t words = scan_words(cut);
                 k_scan_clear<<<grid_for(std::max(words / 4, cut.tiles * kWave), kBlock, 2048), kBlock, 0,
                                stream>>>(p, words, Shape<DT, GRAD>::kTileRows);
+                PDB_LAUNCHED();
             }
             const bool few = cut.tiles > kReach && cut.strips <= (GRAD ? kFewStripsBack : kFewStrips);
-            if constexpr (GRAD) {
-                if (few)
-                    k_scan_grad<DT, W, kFarReach><<<grid, kBlock, 0, stream>>>(p);
-                else
-                    k_scan_grad<DT, W, kReach><<<grid, kBlock, 0, stream>>>(p);
-            } else {
-                if (few)
-                    k_scan<DT, W, kFarReach><<<grid, kBlock, 0, stream>>>(p);
-                else
-                    k_scan<DT, W, kReach><<<grid, kBlock, 0, stream>>>(p);
+            // the counter deals on from launch to launch
+            for (int64_t left = cut.tiles * cut.strips; left > 0; left -= kAtOnce) {
+                const unsigned grid = (unsigned)std::min(left, kAtOnce);
+                if constexpr (GRAD) {
+                    if (few)
+                        k_scan_grad<DT, W, kFarReach><<<grid, kBlock, 0, stream>>>(p);
+                    else
+                        k_scan_grad<DT, W, kReach><<<grid, kBlock, 0, stream>>>(p);
+                } else {
+                    if (few)
+                        k_scan<DT, W, kFarReach><<<grid, kBlock, 0, stream>>>(p);
+                    else
+                        k_scan<DT, W, kReach><<<grid, kBlock, 0, stream>>>(p);
+                }
+                PDB_LAUNCHED();
             }
-            PDB_LAUNCHED();
             return PDB_OK;
         };
         return p.d >= Elem<DT>::kVec ? go(std::true_type()) : go(std::false_type());
