@@ -48,8 +48,9 @@ int pdb_gated_scan_workspace_bytes(int64_t n, int64_t d, size_t *bytes);
  * take the input.
  * n, d, b < 2^31.  ws: at least pdb_gated_scan_workspace_bytes(n, d), aligned to 8,
  * for this call alone until it has run; NULL in the decoding step (n = b, no starts).
- * Tiles of rows pass their states through it: a wait of 20 s there, which only a
- * workspace that something else writes brings about, ends with NaN and *status =
+ * Tiles of rows pass their states through it.  Where something else writes there
+ * meanwhile (another call with the same workspace), what is written is unspecified, but
+ * nothing outside the outputs, and a wait ends after 20 s, with NaN and *status =
  * PDB_ERR_DEVICE. */
 int pdb_gated_scan(const void *x, int64_t ldx, const void *gate, int64_t ldg, int dtype, int64_t n,
                    int64_t d, const int32_t *starts, int64_t b, const float *h0, void *y,

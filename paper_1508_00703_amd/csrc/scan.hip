@@ -421,6 +421,21 @@ constexpr int64_t kFewStrips = 2, kFewStripsBack = 4;
 constexpr int64_t kPatience = 2000000000;  // ticks of the 100 MHz clock: 20 s
 constexpr int64_t kUneasy = 100000;       // 1 ms
 
+// What a tile's place and edges are found by comes from the workspace.  Where something
+// else has written there nothing promises its values, so neither is taken further than the
+// matrices and offsets reach: a place behind the last tile ends the block, with a status,
+// rows behind n are never taken as rows without edges, and no offset is before the first;
+// one wave reads them, so that the block's waves take one path.
+__device__ __forceinline__ bool on_grid(const Scan &p, uint32_t dealt) {
+    if (dealt < (uint32_t)p.tiles * (uint32_t)p.strips) return true;
+    if (p.status && threadIdx.x == 0) *p.status = PDB_ERR_DEVICE;
+    return false;
+}
+__device__ __forceinline__ int32_t first_of(const Scan &p, int tile, int64_t r0, int rows) {
+    const int32_t first = p.first[tile];
+    return first == kPlain && r0 + rows <= p.n ? kPlain : max(first, 0);
+}
+
 template <typename T>
 __device__ __forceinline__ T peek(const T *at) {
     return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -589,12 +604,20 @@ __global__ __launch_bounds__(kBlock, 2) void k_scan(Scan p) {
         }
     }
     __syncthreads();
-    const At at(p, __builtin_amdgcn_readfirstlane(e.dealt));
-    const int32_t first = p.ticket ? p.first[at.tile] : e.first;
+    const uint32_t dealt = __builtin_amdgcn_readfirstlane(e.dealt);
+    if (!on_grid(p, dealt)) return;
+    const At at(p, dealt);
+    int32_t first = 0;
+    if (p.ticket && wave == 0) first = first_of(p, at.tile, at.r0, S::kTileRows);
     u32x4 rx[R], rg[R];
     load_rows<DT, WIDE>(p, p.gate, p.ldg, at.row, at.c0, at.act, rg);
     load_rows<DT, WIDE>(p, p.x, p.ldx, at.row, at.c0, at.act, rx);
-    bool plain = __builtin_amdgcn_readfirstlane(first) == kPlain;
+    if (p.ticket) {
+        if (threadIdx.x == 0) e.first = first;
+        Team<kWaves>::sync_lds();
+    }
+    first = __builtin_amdgcn_readfirstlane(e.first);
+    bool plain = first == kPlain;
     if (!plain) {
         if (wave == 1)
             find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.strip, p.h0, first, e);
@@ -699,8 +722,11 @@ __global__ __launch_bounds__(kBlock, REACH == kReach ? 3 : 2) void k_scan_grad(S
         }
     }
     __syncthreads();
-    const At at(p, __builtin_amdgcn_readfirstlane(e.dealt));
-    const int32_t first = p.ticket ? p.first[at.tile] : e.first;
+    const uint32_t dealt = __builtin_amdgcn_readfirstlane(e.dealt);
+    if (!on_grid(p, dealt)) return;
+    const At at(p, dealt);
+    int32_t first = 0;
+    if (p.ticket && wave == 0) first = first_of(p, at.tile, at.r0, S::kTileRows);
     const int64_t ch = channel_of<V, WIDE>(p, at.strip, slot_of<V>(), false);
     const float mark =
         ch >= 0 && at.r0 < p.n ? p.marks_in[at.r0 / PDB_SCAN_MARK * p.d + ch] : 0.0f;
@@ -708,7 +734,12 @@ __global__ __launch_bounds__(kBlock, REACH == kReach ? 3 : 2) void k_scan_grad(S
     load_rows<DT, WIDE>(p, p.gate, p.ldg, at.row, at.c0, at.act, rg);
     load_rows<DT, WIDE>(p, p.x, p.ldx, at.row, at.c0, at.act, rx);
     load_rows<DT, WIDE>(p, p.dy, p.lddy, at.row, at.c0, at.act, ry);
-    bool plain = __builtin_amdgcn_readfirstlane(first) == kPlain;
+    if (p.ticket) {
+        if (threadIdx.x == 0) e.first = first;
+        Team<kWaves>::sync_lds();
+    }
+    first = __builtin_amdgcn_readfirstlane(e.first);
+    bool plain = first == kPlain;
     if (!plain) {
         if (wave == 1)
             find_edges<V, WIDE>(p, at.r0, at.tile == p.tiles - 1, at.strip, p.d_state, first, e);
