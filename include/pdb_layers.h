@@ -101,8 +101,10 @@ int pdb_grad_norm(const pdb_tensor *grads, int64_t count, float scale, float *no
  * or, with accumulate = 1, that added to what out_i holds (clipped gradient
  * descent: out the parameters, step = -lr).  outs: host array of `count` tensors,
  * each with its gradient's rows and columns, of any of the types; an out may be
- * its gradient (same pointer, type and row stride), and no out may be another's.  The factor is rounded to
- * binary32 once, and the result to out's type.  max_norm >= 0 or +inf; step
+ * its gradient (same pointer, type and row stride), and shares memory with nothing
+ * else that the call reads or writes: PDB_ERR_INVALID_ARG where a tensor without gaps,
+ * or the first row of one with, meets another's.  The factor is rounded to binary32
+ * once, and the result to out's type.  max_norm >= 0 or +inf; step
  * finite.  Where norm[0] is not finite nothing is written but norm[0]; where the
  * factor is 1 an out that is its gradient is not written.  ws: at least
  * pdb_grad_workspace_bytes(). */

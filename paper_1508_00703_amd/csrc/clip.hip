@@ -11,7 +11,9 @@
 // Clipping cannot begin before the last gradient is read: a second pass, from the last
 // chunk to the first, so that it meets first what the cache still holds.
 #include <math.h>
+#include <stdlib.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "pdb_vec.h"
@@ -297,6 +299,48 @@ bool no_gaps(const pdb_tensor *grads, const pdb_tensor *outs, int64_t i) {
     return no_gaps(grads[i]) && (!outs || no_gaps(outs[i]));
 }
 
+// Memory that the call reads or writes: a tensor without gaps, or the first row of one
+// with (rows of several tensors may lie between one another).
+struct Span {
+    uintptr_t at, end;
+    bool written;
+};
+// What the tensors lie in: an output that is its own gradient once.
+int64_t spans_of(const pdb_tensor *grads, const pdb_tensor *outs, int64_t count, Span *spans) {
+    int64_t n = 0;
+    auto add = [&](const pdb_tensor &t, bool written) {
+        const uintptr_t at = (uintptr_t)t.data;
+        const int64_t cells = no_gaps(t) ? t.rows * t.cols : t.cols;
+        spans[n++] = {at, at + (uintptr_t)cells * (uintptr_t)dtype_size(t.dtype), written};
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        if (grads[i].rows == 0 || grads[i].cols == 0) continue;
+        add(outs[i], true);
+        if (grads[i].data != outs[i].data) add(grads[i], false);
+    }
+    return n;
+}
+// Whether an output shares memory with another output or with a gradient that is not its
+// own: the blocks of a launch, and launches one after another, read the gradients while
+// outputs are written, in no order that a caller knows.
+int check_apart(const pdb_tensor *grads, const pdb_tensor *outs, int64_t count) {
+    constexpr int64_t kHere = 256;  // spans that need no memory of their own
+    Span here[kHere];
+    Span *spans = 2 * count <= kHere ? here : static_cast<Span *>(malloc(2 * count * sizeof(Span)));
+    if (!spans) return PDB_ERR_UNSUPPORTED;
+    const int64_t n = spans_of(grads, outs, count, spans);
+    std::sort(spans, spans + n, [](const Span &a, const Span &b) { return a.at < b.at; });
+    uintptr_t read = 0, written = 0;  // how far what was met reaches
+    bool apart = true;
+    for (int64_t i = 0; i < n && apart; ++i) {
+        const Span &s = spans[i];
+        apart = s.at >= written && (!s.written || s.at >= read);
+        (s.written ? written : read) = std::max(s.written ? written : read, s.end);
+    }
+    if (spans != here) free(spans);
+    return apart ? PDB_OK : PDB_ERR_INVALID_ARG;
+}
+
 inline void put(Item &t, const pdb_tensor &g, const pdb_tensor *o, int64_t *chunks) {
     t.rows = (int32_t)g.rows, t.cols = g.cols, t.ld = g.ld, t.ldo = o ? o->ld : 0;
     t.rows_at_once = t.cols >= kChunk ? 1 : (int32_t)(kChunk / t.cols);
@@ -425,6 +469,7 @@ extern "C" int pdb_grad_clip(const pdb_tensor *grads, int64_t count, float scale
                              void *ws, size_t ws_bytes, hipStream_t stream) {
     if (count > 0 && !outs) return PDB_ERR_INVALID_ARG;
     if (int e = check_tensors(grads, count, outs)) return e;
+    if (int e = check_apart(grads, outs, count)) return e;
     if (!isfinite(scale) || !isfinite(step) || !(max_norm >= 0.0f) || !norm || !aligned_to(norm, 4) ||
         (accumulate != 0 && accumulate != 1))
         return PDB_ERR_INVALID_ARG;

@@ -1107,7 +1107,8 @@ def pdb_grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, step: fl
     """step * scale * min(1, max_norm / norm) times the gradients, written to the
     tensors out (None: in place) or, with accumulate, added to them (the parameters
     and step = -lr: the clipped step); the norm, as pdb_grad_norm gives it.  Nothing is
-    written where that is not finite."""
+    written where that is not finite.  An output may be its own gradient, and shares memory
+    with nothing else."""
     grads, dev = _grads(grads)
     out = grads if out is None else list(out)
     if out is not grads and list(map(_SHAPE_OF, out)) != list(map(_SHAPE_OF, grads)):
