@@ -14,14 +14,14 @@
 // and selects keep the mark), and nothing of another sequence passes it, not even a NaN.
 //
 // The bound is the bytes.  131,072 rows of 1,024 channels in 16 bits take 168 us, 4.8 TB/s
-// (in launches that read the rows twice: 504), the gradient's 65,536 156 us, 4.3 TB/s.
+// (in launches that read the rows twice: 504), the gradient's 65,536 158 us, 4.2 TB/s.
 // What stands before the bytes:
 // * waiting: for a tile's loads, its join, and the chain.  Without the chain's waits the
-//   same rows took as long, but 32,768 of 2,048 channels 95 us where they take 102, since a
-//   late tile delays those behind it.  Tiles of half the rows took a third longer, the
+//   same rows took as long, but 32,768 of 2,048 channels 95 us where they took 102 (99 now),
+//   since a late tile delays those behind it.  Tiles of half the rows took a third longer, the
 //   latencies being a tile's whatever its size.
-// * the vector unit, 12 operations and two transcendental ones an element and pass: gates
-//   that cost nothing would save 10 us of the 102.
+// * the vector unit, 13 operations and two transcendental ones an element and pass: gates
+//   that cost nothing would have saved 10 us of the 102.
 // * registers: two numbers an element (the map behind each row) keep the forward pass of 16
 //   bits at two blocks a unit.  Loading the next tile's rows under the chain, or keeping
 //   x and gate and computing gates twice, for three blocks, gained nothing.
@@ -35,8 +35,9 @@ namespace {
 constexpr int kStripLanes = 8;                   // lanes over 128 bytes of a row
 constexpr int kRowLanes = kBlock / kStripLanes;  // 32
 
-// Rows of a thread: two numbers an element, in the backward four.  (In the backward, eight
-// rows of 16 bits spill: 237 us where four take 160.)
+// Rows of a thread: two numbers an element, in the backward four.  (In the backward of 16
+// bits four rows spill 15 registers at three blocks a unit, and take 161 us; at two blocks,
+// without spills, 178; eight rows 237.)
 template <int DT, bool BACK>
 struct Shape {
     static constexpr int V = Elem<DT>::kVec;
